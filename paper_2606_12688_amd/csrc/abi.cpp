@@ -16,32 +16,11 @@
 #include <vector>
 
 #include "mstar_attn.h"
-#include "kernels.h"
-#include "planner.h"
+#include "plan.h"
 
-#define MSTAR_EXPORT extern "C" __attribute__((visibility("default")))
+using mstar::PlanBlock;
 
 namespace {
-
-// Device-side resources of one plan: the device copy of the plan blob, its
-// pinned staging copy, the events that order their reuse, and (for plans that
-// run the few-row kernel beside the tile kernel) a side stream with its fork
-// and join events.  Blocks are pooled per device: a destroyed plan returns its
-// block and later plans take it back, so steady-state planning calls no
-// hipMalloc / hipHostMalloc / hipFree (hipFree would also synchronize the
-// device) and plan destruction makes no HIP call at all.
-struct PlanBlock {
-    int device = -1;
-    size_t bytes = 0;          // capacity of dev and pinned
-    void* dev = nullptr;
-    void* pinned = nullptr;
-    hipEvent_t uploaded = nullptr;  // after the last upload from `pinned`
-    hipEvent_t last_use = nullptr;  // after the last fwd / kv_append enqueued outside graph capture
-    bool uploaded_set = false, last_use_set = false;
-    hipEvent_t ready = nullptr;     // the async planner's upload-done event
-    hipStream_t side = nullptr;     // few-row kernel beside the tile kernel (default priority)
-    hipEvent_t fork = nullptr, join = nullptr;
-};
 
 constexpr size_t kMinBlockBytes = 64 << 10;
 constexpr size_t kPoolMaxBlocks = 64;  // free blocks kept; more are released
@@ -139,23 +118,9 @@ void give_host(mstar::HostPlan& h) {
 
 }  // namespace
 
-struct mstar_plan {
-    mstar::HostPlan host;
-    PlanBlock* blk = nullptr;  // device resources (NULL for a host-only plan)
-    void* dev = nullptr;       // blk->dev
-    size_t bytes = 0;
-    size_t off_seqs = 0, off_row_hi = 0, off_tiles = 0, off_order = 0, off_few = 0, off_f32 = 0, off_merge = 0, off_append = 0, off_casc = 0, off_casc_rows = 0, off_casc_order = 0, off_err = 0;
-    double plan_us = 0.0;
-    // A plan with both tile and few-row items runs the few-row kernel on
-    // blk->side beside the tile kernel: the caller's stream forks at blk->fork
-    // and joins at blk->join before the merge.
-    bool forked = false;
-    bool from_planner = false;  // built by an async planner: blk->ready marks its upload
-};
+namespace mstar {
 
-namespace {
-
-thread_local std::string g_err;
+static thread_local std::string g_err;
 
 int fail(int code, const std::string& msg) {
     g_err = msg;
@@ -166,12 +131,6 @@ int hip_fail(hipError_t e, const char* what) {
     return fail(MSTAR_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// The event that marks `plan`'s device blob as read by work enqueued on `s` (a
-// later plan reusing the block waits for it): it goes with the call's last
-// kernel.  NULL while `s` is being captured into a graph: a capture's replays
-// are the caller's to finish before the plan is destroyed.
 hipError_t use_event(const mstar_plan* plan, hipStream_t s, hipEvent_t* ev) {
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
     const hipError_t e = hipStreamIsCapturing(s, &st);
@@ -179,9 +138,13 @@ hipError_t use_event(const mstar_plan* plan, hipStream_t s, hipEvent_t* ev) {
     return e;
 }
 
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+}  // namespace mstar
 
-}  // namespace
+using mstar::align256;
+using mstar::aligned;
+using mstar::fail;
+using mstar::hip_fail;
+using mstar::use_event;
 
 static int plan_impl(const mstar_attn_params* params, const mstar_seq_desc* seqs, const mstar_mask_spec* masks,
                      int32_t num_seqs, const mstar_segment* segments, int32_t num_segs,
@@ -336,17 +299,10 @@ MSTAR_EXPORT size_t mstar_attn_workspace_bytes(const mstar_plan_t* plan) {
     return align256(slots * plan->host.params.head_dim * sizeof(float)) + align256(slots * sizeof(float));
 }
 
-MSTAR_EXPORT int mstar_attn_fwd(const mstar_plan_t* plan, const void* q, const void* k_pages,
-                                const void* v_pages, const int32_t* block_table, void* out, float* lse,
-                                void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    return mstar_attn_fwd_timed(plan, q, k_pages, v_pages, block_table, out, lse, workspace, workspace_bytes,
-                                stream, nullptr, nullptr);
-}
-
-MSTAR_EXPORT int mstar_attn_fwd_timed(const mstar_plan_t* plan, const void* q, const void* k_pages,
-                                      const void* v_pages, const int32_t* block_table, void* out, float* lse,
-                                      void* workspace, size_t workspace_bytes, hipStream_t stream,
-                                      const hipEvent_t* events_before, const hipEvent_t* events_after) {
+int mstar::run_fwd(const Launchers& kernels, const mstar_plan* plan, const void* q, const void* k_pages,
+                   const void* v_pages, const int32_t* block_table, void* out, float* lse, void* workspace,
+                   size_t workspace_bytes, hipStream_t stream, const hipEvent_t* events_before,
+                   const hipEvent_t* events_after) {
     if (!plan) return fail(MSTAR_ERR_INVALID_ARG, "plan is NULL");
     if (!plan->dev) return fail(MSTAR_ERR_INVALID_ARG, "plan was built host-only");
     const mstar::HostPlan& h = plan->host;
@@ -419,7 +375,7 @@ MSTAR_EXPORT int mstar_attn_fwd_timed(const mstar_plan_t* plan, const void* q, c
         a.n_items = (int32_t)h.few.size();
         a.done = done(1);
         MSTAR_MARK(events_before, 1);
-        if ((e = mstar::launch_few(a, D, h.decode_rb, s_few)) != hipSuccess) return hip_fail(e, "few-row kernel launch");
+        if ((e = kernels.few(a, D, h.decode_rb, s_few)) != hipSuccess) return hip_fail(e, "few-row kernel launch");
         MSTAR_MARK(events_after, 1);
     }
     if (side) {
@@ -434,7 +390,7 @@ MSTAR_EXPORT int mstar_attn_fwd_timed(const mstar_plan_t* plan, const void* q, c
         a.span_step = std::max(512, h.tile_span / 4);
         a.done = done(0);
         MSTAR_MARK(events_before, 0);
-        if ((e = mstar::launch_tiles(a, D, s)) != hipSuccess) return hip_fail(e, "tile kernel launch");
+        if ((e = kernels.tiles(a, D, s)) != hipSuccess) return hip_fail(e, "tile kernel launch");
         MSTAR_MARK(events_after, 0);
     }
     if (!h.cascade.empty()) {
@@ -447,7 +403,7 @@ MSTAR_EXPORT int mstar_attn_fwd_timed(const mstar_plan_t* plan, const void* q, c
         a.rows = reinterpret_cast<const int32_t*>(blob + plan->off_casc_rows);
         a.done = done(4);
         MSTAR_MARK(events_before, 4);
-        if ((e = mstar::launch_cascade(a, D, s)) != hipSuccess) return hip_fail(e, "cascade kernel launch");
+        if ((e = kernels.cascade(a, D, s)) != hipSuccess) return hip_fail(e, "cascade kernel launch");
         MSTAR_MARK(events_after, 4);
     }
     if (side) {
@@ -482,9 +438,9 @@ MSTAR_EXPORT int mstar_attn_fwd_timed(const mstar_plan_t* plan, const void* q, c
     return MSTAR_OK;
 }
 
-MSTAR_EXPORT int mstar_attn_fwd_noalloc(const mstar_plan_t* plan, const void* q, const void* k_pages,
-                                        const void* v_pages, const int32_t* block_table, void* out, float* lse,
-                                        hipStream_t stream) {
+int mstar::run_fwd_noalloc(const Launchers& kernels, const mstar_plan* plan, const void* q, const void* k_pages,
+                           const void* v_pages, const int32_t* block_table, void* out, float* lse,
+                           hipStream_t stream) {
     if (!plan) return fail(MSTAR_ERR_INVALID_ARG, "plan is NULL");
     const size_t need = mstar_attn_workspace_bytes(plan);
     if (need > mstar::kScratchBytes)
@@ -498,8 +454,33 @@ MSTAR_EXPORT int mstar_attn_fwd_noalloc(const mstar_plan_t* plan, const void* q,
         hipError_t e = mstar::scratch_buffer(&ws);
         if (e != hipSuccess) return hip_fail(e, "scratch address");
     }
-    return mstar_attn_fwd_timed(plan, q, k_pages, v_pages, block_table, out, lse, ws, need > 0 ? mstar::kScratchBytes : 0,
-                                stream, nullptr, nullptr);
+    return run_fwd(kernels, plan, q, k_pages, v_pages, block_table, out, lse, ws, need > 0 ? kScratchBytes : 0, stream,
+                   nullptr, nullptr);
+}
+
+namespace {
+constexpr mstar::Launchers kKernels = {mstar::launch_tiles, mstar::launch_few, mstar::launch_cascade};
+}
+
+MSTAR_EXPORT int mstar_attn_fwd(const mstar_plan_t* plan, const void* q, const void* k_pages,
+                                const void* v_pages, const int32_t* block_table, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    return mstar::run_fwd(kKernels, plan, q, k_pages, v_pages, block_table, out, lse, workspace, workspace_bytes,
+                          stream, nullptr, nullptr);
+}
+
+MSTAR_EXPORT int mstar_attn_fwd_timed(const mstar_plan_t* plan, const void* q, const void* k_pages,
+                                      const void* v_pages, const int32_t* block_table, void* out, float* lse,
+                                      void* workspace, size_t workspace_bytes, hipStream_t stream,
+                                      const hipEvent_t* events_before, const hipEvent_t* events_after) {
+    return mstar::run_fwd(kKernels, plan, q, k_pages, v_pages, block_table, out, lse, workspace, workspace_bytes,
+                          stream, events_before, events_after);
+}
+
+MSTAR_EXPORT int mstar_attn_fwd_noalloc(const mstar_plan_t* plan, const void* q, const void* k_pages,
+                                        const void* v_pages, const int32_t* block_table, void* out, float* lse,
+                                        hipStream_t stream) {
+    return mstar::run_fwd_noalloc(kKernels, plan, q, k_pages, v_pages, block_table, out, lse, stream);
 }
 
 MSTAR_EXPORT int mstar_kv_append(const mstar_plan_t* plan, const void* k_new, const void* v_new,
@@ -552,7 +533,9 @@ MSTAR_EXPORT int mstar_attn_check(mstar_plan_t* plan, hipStream_t stream, int32_
         const int32_t zero = 0;
         e = hipMemcpy(d_err, &zero, sizeof zero, hipMemcpyHostToDevice);
         if (e != hipSuccess) return hip_fail(e, "error word clear");
-        return fail(MSTAR_ERR_INVALID_ARG, "a block-table entry was outside [0, num_pages)");
+        return fail(MSTAR_ERR_INVALID_ARG, (v & MSTAR_DEVERR_PAGE_RANGE)
+                                               ? "a block-table entry was outside [0, num_pages)"
+                                               : "a new key or value was infinite or not a number");
     }
     return MSTAR_OK;
 }
@@ -642,7 +625,7 @@ MSTAR_EXPORT void mstar_attn_plan_destroy(mstar_plan_t* plan) {
     delete plan;
 }
 
-MSTAR_EXPORT const char* mstar_last_error(void) { return g_err.c_str(); }
+MSTAR_EXPORT const char* mstar_last_error(void) { return mstar::g_err.c_str(); }
 
 // ---------------------------------------------------------------------------
 // Async planner: plans built in submission order on a worker thread that owns
