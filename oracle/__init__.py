@@ -15,7 +15,8 @@ this computation through a paged-attention library inside its
 tables are read in place (Sec. 4.1); it does not define the masks, so the
 mask semantics are the reading stated in ``attention.py``.  ``append.py``
 holds the paged KV append (the step's new K/V rows written into their pages
-before attention reads them).
+before attention reads them), ``kv4.py`` the 4-bit cache's rounding and layout
+and the block tables.
 
 Pins (tests marked ``not gpu``): brute-force visibility predicates written from
 each workload's wording, torch's CPU float64 ``scaled_dot_product_attention``
@@ -39,3 +40,10 @@ from .attention import (  # noqa: F401
     visible_matrix,
 )
 from .append import append_targets, kv_append  # noqa: F401
+from .kv4 import (  # noqa: F401
+    block_tables,
+    kv4_append,
+    kv4_read,
+    kv4_round,
+    kv4_values,
+)

@@ -17,7 +17,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmstar_attn.so")
-SOURCES = ["abi.cpp", "planner.cpp", "kernels.hip"]
+SOURCES = ["abi.cpp", "abi_cache.cpp", "planner.cpp", "kernels.hip", "kernels_cache.hip"]
 
 
 def hipcc() -> str:

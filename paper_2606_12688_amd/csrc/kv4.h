@@ -1,0 +1,43 @@
+// Device code of the 4-bit cache: where a record keeps a key's codes and
+// scales, and how codes become bf16 values.  The layout is that of
+// mstar_cache.h; in a wave's terms (lane l = 16 G + n) a lane's D / 8 bytes of
+// a record are, for K, dims [G D / 4, (G + 1) D / 4) of key n, and for V, dims
+// [n D / 16, (n + 1) D / 16) of keys 4 G .. 4 G + 3.
+#pragma once
+#include "cache.h"
+#include "device.h"
+
+namespace mstar {
+namespace {
+
+typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int MSTAR_DEVERR_NONFINITE_BIT = MSTAR_DEVERR_NONFINITE;
+constexpr int kScaleMin = 2, kScaleMax = 252;  // scale bytes: every value is a normal, finite bf16 number
+
+template <int D>
+struct Record {
+    static constexpr int kBytes = MSTAR_KV4_RECORD_BYTES(D);
+    static constexpr int kScales = 8 * D;   // offset of the scale bytes
+    static constexpr int kWord = D / 32;    // bytes of D / 16 dims of one key: what lane n holds of a row
+    // word n (dims [n D / 16, +D / 16)) of key `slot`
+    __device__ __forceinline__ static int k_word(int slot, int n) {
+        return ((n >> 2) * 16 + slot) * (D / 8) + (n & 3) * kWord;
+    }
+    __device__ __forceinline__ static int v_word(int slot, int n) {
+        return (((slot >> 2) * 16 + n) * 4 + (slot & 3)) * kWord;
+    }
+    __device__ __forceinline__ static int scale(int slot, int n) { return kScales + (n * (D / 16) / 32) * 16 + slot; }
+};
+
+// The scale byte as the fp32 operand of the conversions, which use its exponent.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Byte B of `w` as two bf16 values.
+template <int B>
+__device__ __forceinline__ bf16x2 pair_of(uint32_t w, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B);
+}
+
+}  // namespace
+}  // namespace mstar

@@ -19,7 +19,8 @@ constexpr int kAppendRows = 16;    // new K/V rows per KV-append item
 // lo(i) = window ? max(0, position - window + 1) : 0.
 struct SeqInfo {
     int32_t q_len, kv_len, q_start, window;
-    int32_t hi_off, seq_index, pad0, pad1;
+    int32_t hi_off, seq_index;
+    int32_t page_off, pad0;  // new pages of the requests before (block tables)
 };
 
 // A unit of work over key range [k_begin, k_end).

@@ -277,7 +277,9 @@ int build_host_plan(const mstar_attn_params* params, const mstar_seq_desc* seqs,
         si.window = masks[r].window;
         si.hi_off = (int32_t)plan.row_hi.size();
         si.seq_index = r;
-        si.pad0 = si.pad1 = 0;
+        si.page_off = (int32_t)plan.new_pages;
+        si.pad0 = 0;
+        plan.new_pages += ceil_div(s.kv_len, kPage) - ceil_div(s.kv_len - s.q_len, kPage);
         plan.row_hi.resize(plan.row_hi.size() + s.q_len);
         int32_t* hi = plan.row_hi.data() + si.hi_off;
         int64_t pairs = 0;

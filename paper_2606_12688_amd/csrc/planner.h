@@ -36,6 +36,7 @@ struct HostPlan {
     bool key_groups = false;  // multi-row kernel: the waves of a CU share each workgroup's keys
     int64_t visible_pairs = 0;
     int64_t partial_slots = 0;
+    int64_t new_pages = 0;  // pages that the new rows start, over all requests
 
     // Back to the state of a new HostPlan, keeping the vectors' capacity (a
     // pooled plan then writes into memory it has already touched).  Every
@@ -50,7 +51,7 @@ struct HostPlan {
         merges.clear();
         tile_span = casc_span = 0;
         key_groups = false;
-        visible_pairs = partial_slots = 0;
+        visible_pairs = partial_slots = new_pages = 0;
     }
     // Bytes the vectors hold (their capacity).
     size_t capacity_bytes() const {
