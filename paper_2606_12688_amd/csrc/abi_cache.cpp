@@ -31,6 +31,8 @@ int check_plan4(const mstar_plan* plan) {
     return MSTAR_OK;
 }
 
+constexpr mstar::Launchers kKernels4 = {mstar::launch_tiles4, mstar::launch_few4, mstar::launch_cascade4};
+
 template <typename T>
 T* at(const mstar_plan* plan, size_t off) {
     return reinterpret_cast<T*>(static_cast<unsigned char*>(plan->dev) + off);
@@ -75,41 +77,8 @@ MSTAR_EXPORT int mstar_kv4_fwd(const mstar_plan_t* plan, const void* q, const vo
                                size_t workspace_bytes, hipStream_t stream) {
     const int rc = check_plan4(plan);
     if (rc != MSTAR_OK) return rc;
-    const mstar::HostPlan& h = plan->host;
-    if (h.appends.empty()) return MSTAR_OK;
-    if (!q || !k_pages || !v_pages || !block_table || !out || !lse)
-        return fail(MSTAR_ERR_INVALID_ARG, "a tensor pointer is NULL");
-    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) ||
-        !aligned(lse, 4) || !aligned(block_table, 4))
-        return fail(MSTAR_ERR_INVALID_ARG, "q/k_pages/v_pages/out must be 16-byte aligned");
-    const size_t need = mstar_attn_workspace_bytes(plan);
-    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))
-        return fail(MSTAR_ERR_WORKSPACE, "workspace missing, misaligned or smaller than mstar_attn_workspace_bytes");
-    mstar::KArgs a{};
-    a.seqs = at<const mstar::SeqInfo>(plan, plan->off_seqs);
-    a.row_hi = at<const int32_t>(plan, plan->off_row_hi);
-    a.items = at<const mstar::WorkItem>(plan, plan->off_append);
-    a.n_items = (int32_t)h.appends.size();
-    a.q = q;
-    a.k = k_pages;
-    a.v = v_pages;
-    a.bt = block_table;
-    a.out = out;
-    a.lse = lse;
-    a.err = at<int32_t>(plan, plan->off_err);
-    a.hq = h.params.num_qo_heads;
-    a.hkv = h.params.num_kv_heads;
-    a.group = h.group;
-    a.bt_stride = h.params.max_blocks_per_seq;
-    a.num_pages = h.params.num_pages;
-    a.sm_scale = h.params.sm_scale;
-    a.scale_log2 = h.params.sm_scale * 1.4426950408889634f;
-    hipError_t e = mstar::use_event(plan, stream, &a.done);
-    if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
-    if ((e = mstar::launch_rows4(a, h.params.head_dim, stream)) != hipSuccess)
-        return hip_fail(e, "4-bit attention kernel launch");
-    if (a.done) plan->blk->last_use_set = true;
-    return MSTAR_OK;
+    return mstar::run_fwd(kKernels4, plan, q, k_pages, v_pages, block_table, out, lse, workspace, workspace_bytes,
+                          stream, nullptr, nullptr);
 }
 
 MSTAR_EXPORT int mstar_kv4_fwd_noalloc(const mstar_plan_t* plan, const void* q, const void* k_pages,
@@ -117,12 +86,7 @@ MSTAR_EXPORT int mstar_kv4_fwd_noalloc(const mstar_plan_t* plan, const void* q, 
                                        hipStream_t stream) {
     const int rc = check_plan4(plan);
     if (rc != MSTAR_OK) return rc;
-    const size_t need = mstar_attn_workspace_bytes(plan);
-    if (need > mstar::kScratchBytes) return fail(MSTAR_ERR_WORKSPACE, "the plan needs more scratch than the library holds");
-    void* ws = nullptr;
-    const hipError_t e = need > 0 ? mstar::scratch_buffer(&ws) : hipSuccess;
-    if (e != hipSuccess) return hip_fail(e, "scratch address");
-    return mstar_kv4_fwd(plan, q, k_pages, v_pages, block_table, out, lse, ws, need, stream);
+    return mstar::run_fwd_noalloc(kKernels4, plan, q, k_pages, v_pages, block_table, out, lse, stream);
 }
 
 MSTAR_EXPORT int mstar_kv4_unpack(int32_t num_kv_heads, int32_t head_dim, int32_t num_pages, const void* k_pages,

@@ -46,6 +46,8 @@ hipError_t launch_unpack4(const Unpack4Args& a, int head_dim, hipStream_t s);
 hipError_t launch_tables(const TablesArgs& a, hipStream_t s);
 
 // Attention over a 4-bit cache: k and v of KArgs are 4-bit pools.
-hipError_t launch_rows4(const KArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_tiles4(const KArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_cascade4(const KArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_few4(const KArgs& a, int head_dim, int row_blocks, hipStream_t s);
 
 }  // namespace mstar

@@ -273,6 +273,8 @@ __device__ __forceinline__ void lds_dma4(__amdgpu_buffer_rsrc_t r, uint32_t voff
 __device__ __forceinline__ void dma_barrier() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+// The same without the wait for loads: for tiles that waves write into LDS themselves.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 typedef __attribute__((address_space(3))) char lds_char;
 
 // Waits until at most N vector memory operations of this wave are outstanding.
@@ -319,7 +321,7 @@ __device__ __forceinline__ void lds_dma16s(__amdgpu_buffer_rsrc_t r, uint32_t vo
 // K/V of a pool that fits in 2 GB are read through one buffer resource per
 // pool with the page's byte offset in the instruction's scalar offset, so a
 // load costs no scalar work beyond one multiply per page.  Larger pools get a
-// resource per page (SMALL = false).  The 2 GB resource range keeps every
+// resource per page.  The 2 GB resource range keeps every
 // valid offset in range and pushes the marker offset below out of range.
 constexpr uint32_t kSmallPoolBytes = 0x80000000u;
 

@@ -781,12 +781,12 @@ hipError_t launch_tile_mode(const KArgs& a, int head_dim, hipStream_t s) {
     const bool small = small_pool(a, head_dim);
     if (head_dim == 64) {
         const dim3 b(256 * KS64);
-        if (small) return launch(tile_kernel<64, 2, true, MODE, 64, KS64>, g, b, a, s);
-        else return launch(tile_kernel<64, 2, false, MODE, 64, KS64>, g, b, a, s);
+        if (small) return launch(tile_kernel<64, 2, kPoolSmall, MODE, 64, KS64>, g, b, a, s);
+        else return launch(tile_kernel<64, 2, kPoolLarge, MODE, 64, KS64>, g, b, a, s);
     } else {
         const dim3 b(256 * KS128);
-        if (small) return launch(tile_kernel<128, 2, true, MODE, kTileKeysD128, KS128>, g, b, a, s);
-        else return launch(tile_kernel<128, 2, false, MODE, kTileKeysD128, KS128>, g, b, a, s);
+        if (small) return launch(tile_kernel<128, 2, kPoolSmall, MODE, kTileKeysD128, KS128>, g, b, a, s);
+        else return launch(tile_kernel<128, 2, kPoolLarge, MODE, kTileKeysD128, KS128>, g, b, a, s);
     }
 }
 }  // namespace

@@ -1,6 +1,6 @@
 // HIP kernels of the operators on paged caches (mstar_cache.h) for gfx950: the
 // 4-bit cache's append, attention and read-back, and block tables.
-#include "kv4.h"
+#include "tile.h"
 
 namespace mstar {
 namespace {
@@ -124,88 +124,251 @@ __global__ __launch_bounds__(256) void unpack4_kernel(Unpack4Args a) {
 }
 
 // ---------------------------------------------------------------------------
-// Attention: a wave per (query row, head), a page at a time.  Lane 16 G + n
-// forms its share of key n's score (dims [G D / 4, +D / 4)) and of the values of
-// keys 4 G .. 4 G + 3 (dims [n D / 16, +D / 16)).
+// Few-row attention over a 4-bit cache: the work items, rows and steps of the
+// 16-bit few-row kernel (a workgroup is up to 16 RB rows of one KV head, its
+// waves take interleaved 32-key steps), on other operands.  Both K and V go from
+// the pages straight into matrix operands, with nothing through LDS:
+//  scores: lane 16 G + n holds dims [G D / 4, +D / 4) of key n, so MFMA step s
+//    contracts dims G D / 4 + 8 s .. + 7 of each group G, and Q is read that way;
+//  values: the lane holds dims [n D / 16, +D / 16) of keys 4 G .. 4 G + 3, and
+//    output row m of block db stands for dim m D / 16 + db.  A conversion gives
+//    two dims of one key, an operand register takes two keys of one dim: a byte
+//    permute exchanges the halves.
+// A lane's share of out is then the D / 4 consecutive dims from G D / 4 on.
 // ---------------------------------------------------------------------------
-template <int D>
-__global__ __launch_bounds__(256) void rows4_kernel(KArgs a) {
-    constexpr int EK = D / 4, EV = D / 16;
+template <int D, int RB>
+__global__ __launch_bounds__(256, RB == 1 ? 4 : (D == 64 && RB == 2 ? 3 : 2)) void few4_kernel(KArgs a) {
     typedef Record<D> R;
-    const int item = wg_id() / a.hq, head = wg_id() - item * a.hq;
-    const WorkItem it = a.items[item];
+    constexpr int NW = 4;              // waves
+    constexpr int SK = kSubKeys;       // keys per step: two pages
+    constexpr int DS = D / 32, DB = D / 16;
+    constexpr int NC = D / 32;         // dwords of codes per lane and record
+    constexpr int PC = D / 16;         // 16-byte pieces of a lane's results per row block
+    __shared__ __attribute__((aligned(1024))) f32x4 o_lds[NW][PC * 64];
+    __shared__ float ml_lds[NW][2][RB * 16];
+    __shared__ float fin_lds[2][RB * 16];
+
+    const WorkItem it = a.items[wg_id()];
     const SeqInfo si = a.seqs[it.seq];
-    const int wave = __builtin_amdgcn_readfirstlane(thread_id() >> 6) & 3, lane = thread_id() & 63;
+    const int tid = thread_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6) & (NW - 1), lane = tid & 63;
     const int n = lane & 15, grp = lane >> 4;
+    const int G = a.group;
+    const int kvh = it.head;
     const int32_t* bt_row = a.bt + (int64_t)it.seq * a.bt_stride;
+    const RowGroup rg;
+
+    int32_t lo[RB], hi[RB];
+    bf16x8 qf[RB][DS];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int r = rb * 16 + n;
+        const bool valid = r < it.nrows;
+        const int rr = it.row0 + r;
+        const int qi = rr / G, h = kvh * G + rr % G;
+        lo[rb] = 0;
+        hi[rb] = 0;
+        if (valid) row_interval(a, si, it, qi, lo[rb], hi[rb]);
+        const int64_t qoff = ((int64_t)(si.q_start + qi) * a.hq + h) * D + grp * (D / 4);
+#pragma unroll
+        for (int s = 0; s < DS; ++s)
+            qf[rb][s] = valid ? __builtin_bit_cast(bf16x8, load16(a.q, qoff + 8 * s)) : bf16x8{};
+    }
+    int32_t lo_max, hi_min, dummy;
+    {
+        const int q_first = it.row0 / G, q_last = (it.row0 + it.nrows - 1) / G;
+        row_interval(a, si, it, q_first, dummy, hi_min);
+        row_interval(a, si, it, q_last, lo_max, dummy);
+    }
+
+    float m[RB], l[RB];
+    f32x4 o[RB][DB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = kNegInf;
+        l[rb] = 0.0f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0, 0, 0, 0};
+    }
+
+    // Steps of this wave and their pages as in the 16-bit kernel: step i starts at
+    // key k_begin + 32 (wave + NW i); lane 2 i + h of a window holds half h's page.
+    const int n_steps = (it.k_end - it.k_begin + SK - 1) / SK;
+    const int my_steps = wave < n_steps ? (n_steps - wave + NW - 1) / NW : 0;
+    const int32_t page0 = it.k_begin >> 4;
+    const int32_t n_pages = ((it.k_end + 15) >> 4) - page0;
+    auto load_pages = [&](int first_step) {
+        const int pg = 2 * (wave + NW * (first_step + (lane >> 1))) + (lane & 1);
+        return pg < n_pages ? bt_row[page0 + pg] : -1;
+    };
+    int32_t pw_cur = load_pages(0), pw_next = my_steps > 32 ? load_pages(32) : 0;
+    const char* kbase = reinterpret_cast<const char*>(a.k);
+    const char* vbase = reinterpret_cast<const char*>(a.v);
+    const int koff = R::kScales + (grp * (D / 4) / 32) * 16 + n, voff = R::scale(4 * grp, n);
     bool page_err = false;
-    for (int r = wave; r < it.nrows; r += 4) {
-        const int i = it.row0 + r;
-        const int32_t pos = si.kv_len - si.q_len + i;
-        const int32_t lo = si.window > 0 ? max(0, pos - si.window + 1) : 0, hi = a.row_hi[si.hi_off + i];
-        const int64_t row = (int64_t)(si.q_start + i) * a.hq + head;
-        float q[EK];
+    struct Raw {
+        uint32_t k[2][NC], v[2][NC];  // this lane's codes of the step's two records
+        uint32_t ks[2], vs[2];        // its key's scale byte; those of its four keys
+    };
+    // Pages outside the pool, and past the item's end, read zeros through an empty buffer range.
+    auto load_step = [&](int i, Raw& x) {
+        if (i > 0 && (i & 31) == 0) {  // next window of page indices
+            pw_cur = pw_next;
+            pw_next = i + 32 < my_steps ? load_pages(i + 32) : 0;
+        }
 #pragma unroll
-        for (int e = 0; e < EK; ++e) q[e] = (float)static_cast<const bf16_t*>(a.q)[row * D + grp * EK + e];
-        float m = kNegInf, l = 0.0f, o[EV];
-#pragma unroll
-        for (int e = 0; e < EV; ++e) o[e] = 0.0f;
-        for (int32_t k0 = lo & ~15; k0 < hi; k0 += 16) {
-            const int32_t page = bt_row[k0 >> 4];
+        for (int h = 0; h < 2; ++h) {
+            const int32_t page = __builtin_amdgcn_readlane(pw_cur, 2 * (i & 31) + h);
             const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
-            page_err |= !ok;
-            const int64_t rec = ok ? ((int64_t)page * a.hkv + head / a.group) * R::kBytes : 0;
-            const unsigned char* kr = static_cast<const unsigned char*>(a.k) + rec;
-            const unsigned char* vr = static_cast<const unsigned char*>(a.v) + rec;
-            float s = 0.0f;
-#pragma unroll
-            for (int d = 0; d < EK / 8; ++d) {
-                const uint32_t w = ok ? reinterpret_cast<const uint32_t*>(kr)[lane * (D / 32) + d] : 0;
-                const float sc = scale_of(ok ? kr[R::scale(n, 4 * grp)] : 0);
-                const bf16x2 p0 = pair_of<0>(w, sc), p1 = pair_of<1>(w, sc), p2 = pair_of<2>(w, sc), p3 = pair_of<3>(w, sc);
-                s += q[8 * d] * (float)p0[0] + q[8 * d + 1] * (float)p0[1] + q[8 * d + 2] * (float)p1[0] +
-                     q[8 * d + 3] * (float)p1[1] + q[8 * d + 4] * (float)p2[0] + q[8 * d + 5] * (float)p2[1] +
-                     q[8 * d + 6] * (float)p3[0] + q[8 * d + 7] * (float)p3[1];
+            page_err |= !ok && 2 * (wave + NW * i) + h < n_pages;
+            const size_t ofs = ok ? ((size_t)page * a.hkv + kvh) * R::kBytes : 0;
+            const uint32_t nrec = ok ? (uint32_t)R::kBytes : 0u;
+            const __amdgpu_buffer_rsrc_t rk = page_rsrc(kbase, ofs, nrec), rv = page_rsrc(vbase, ofs, nrec);
+            if constexpr (D == 128) {
+                const uint4 kc = load16_at(rk, lane * 16), vc = load16_at(rv, lane * 16);
+                x.k[h][0] = kc.x; x.k[h][1] = kc.y; x.k[h][2] = kc.z; x.k[h][3] = kc.w;
+                x.v[h][0] = vc.x; x.v[h][1] = vc.y; x.v[h][2] = vc.z; x.v[h][3] = vc.w;
+            } else {
+                typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+                const u32x2 kc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rk, lane * 8, 0, 0));
+                const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rv, lane * 8, 0, 0));
+                x.k[h][0] = kc[0]; x.k[h][1] = kc[1];
+                x.v[h][0] = vc[0]; x.v[h][1] = vc[1];
             }
-            s += __shfl_xor(s, 16, 64);
-            s += __shfl_xor(s, 32, 64);
-            if (k0 + n < lo || k0 + n >= hi) s = kNegInf;
-            float top = s;
-            for (int x = 8; x > 0; x >>= 1) top = fmax_num(top, __shfl_xor(top, x, 64));
-            const float m_new = fmax_num(m, top * a.scale_log2);
-            const float alpha = fast_exp2(m - m_new);
-            m = m_new;
-            const float p = fast_exp2(fmaf(s, a.scale_log2, -m));
-            l = l * alpha + p;
+            x.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rk, koff, 0, 0);
+            x.vs[h] = __builtin_amdgcn_raw_buffer_load_b32(rv, voff, 0, 0);
+        }
+    };
+    auto compute_step = [&](int i, const Raw& x) {
+        const int32_t k0 = it.k_begin + SK * (wave + NW * i);
+        f32x4 sc[RB][2];
 #pragma unroll
-            for (int e = 0; e < EV; ++e) o[e] *= alpha;
+        for (int h = 0; h < 2; ++h) {
+            const float sk = scale_of(x.ks[h]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int slot = 4 * grp + j;
-                const float pj = __shfl(p, slot, 64);
-                uint32_t w = 0, b = 0;
-                if (ok) {
-                    const unsigned char* word = vr + R::v_word(slot, n);
-                    w = D == 128 ? *reinterpret_cast<const uint32_t*>(word) : *reinterpret_cast<const uint16_t*>(word);
-                    b = min((int)vr[R::scale(slot, n)], kScaleMax);
-                }
-                const float sc = scale_of(b);
-                const bf16x2 v[4] = {pair_of<0>(w, sc), pair_of<1>(w, sc), pair_of<2>(w, sc), pair_of<3>(w, sc)};
+            for (int s = 0; s < DS; ++s) {
+                const bf16x8 kf = eight_of(x.k[h][s], sk);
 #pragma unroll
-                for (int e = 0; e < EV; ++e) o[e] = fmaf(pj, (float)v[e >> 1][e & 1], o[e]);
+                for (int rb = 0; rb < RB; ++rb) sc[rb][h] = mfma16(kf, qf[rb][s], s == 0 ? f32x4{0, 0, 0, 0} : sc[rb][h]);
             }
         }
-        for (int x = 8; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
+        if (!(k0 >= lo_max && k0 + SK <= hi_min)) {
 #pragma unroll
-        for (int e = 0; e < EV; ++e) {
-            o[e] += __shfl_xor(o[e], 16, 64);
-            o[e] += __shfl_xor(o[e], 32, 64);
-            o[e] *= l > 0.0f ? 1.0f / l : 0.0f;
-            if (grp == 0) static_cast<bf16_t*>(a.out)[row * D + n * EV + e] = (bf16_t)o[e];
+            for (int rb = 0; rb < RB; ++rb) {
+                const int32_t lo_r = lo[rb] - (k0 + 4 * grp), hi_r = hi[rb] - (k0 + 4 * grp);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int c = h * 16 + e;
+                        if (!(c >= lo_r && c < hi_r)) sc[rb][h][e] = kNegInf;
+                    }
+            }
         }
-        if (lane == 0) a.lse[row] = l > 0.0f ? (m + __log2f(l)) * kLn2 : kNegInf;
+        float alpha[RB];
+        if (softmax_update<RB, 2>(rg, sc, a.scale_log2, m, l, alpha)) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) o[rb][db] *= alpha[rb];
+        }
+        bf16x8 pf[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) pf[rb] = to_bf16x8(sc[rb][0], sc[rb][1]);
+        float sv[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sv[h][j] = scale_of(v_scale(x.vs[h], j));
+#pragma unroll
+        for (int b = 0; b < DB / 2; ++b) {  // dims 2 b and 2 b + 1 of the lane's: blocks 2 b and 2 b + 1
+            uint4 even, odd;
+            uint32_t* ev = &even.x;
+            uint32_t* od = &odd.x;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = __builtin_bit_cast(uint32_t, v_pair<D>(x.v[h], j, b, sv[h][j]));
+                ev[2 * h] = __builtin_amdgcn_perm(y[1], y[0], 0x05040100);
+                ev[2 * h + 1] = __builtin_amdgcn_perm(y[3], y[2], 0x05040100);
+                od[2 * h] = __builtin_amdgcn_perm(y[1], y[0], 0x07060302);
+                od[2 * h + 1] = __builtin_amdgcn_perm(y[3], y[2], 0x07060302);
+            }
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                o[rb][2 * b] = mfma16(__builtin_bit_cast(bf16x8, even), pf[rb], o[rb][2 * b]);
+                o[rb][2 * b + 1] = mfma16(__builtin_bit_cast(bf16x8, odd), pf[rb], o[rb][2 * b + 1]);
+            }
+        }
+    };
+
+    if (my_steps > 0) {
+        Raw next;
+        load_step(0, next);
+        for (int i = 0; i < my_steps; ++i) {
+            const Raw cur = next;
+            if (i + 1 < my_steps) load_step(i + 1, next);
+            compute_step(i, cur);
+        }
     }
     if (page_err && lane == 0) atomicOr(a.err, MSTAR_DEVERR_PAGE_RANGE_BIT);
+
+    // ---- combine the waves ------------------------------------------------------
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const float lt = rg.sum(l[rb]);
+        if (grp == 0) {
+            ml_lds[wave][0][rb * 16 + n] = m[rb];
+            ml_lds[wave][1][rb * 16 + n] = lt;
+        }
+    }
+    __syncthreads();
+    // one row block at a time: each wave leaves its results against the common
+    // reference, 16-byte pieces in lane order, and all threads add them up
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int row = rb * 16 + n;
+        float mstar = kNegInf;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) mstar = fmax_num(mstar, ml_lds[w][0][row]);
+        const float mu = mstar == kNegInf ? 0.0f : mstar;
+        if (wave == 0 && grp == 0) {
+            float L = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) L += fast_exp2(ml_lds[w][0][row] - mu) * ml_lds[w][1][row];
+            fin_lds[0][row] = mstar;
+            fin_lds[1][row] = L;
+        }
+        const float own = fast_exp2(m[rb] - mu);
+        if (rb > 0) __syncthreads();  // the previous block has been added up
+#pragma unroll
+        for (int p = 0; p < PC; ++p) {  // dims G D / 4 + 4 p ..: row r of blocks db .. db + 3
+            const int r = 4 * p / DB, db = 4 * p % DB;
+            o_lds[wave][p * 64 + lane] = f32x4{o[rb][db][r], o[rb][db + 1][r], o[rb][db + 2][r], o[rb][db + 3][r]} * own;
+        }
+        __syncthreads();
+        for (int e = tid; e < PC * 64; e += 64 * NW) {
+            const int r = rb * 16 + (e & 15), d4 = ((e >> 4) & 3) * (D / 4) + 4 * (e >> 6);
+            if (r >= it.nrows) continue;
+            f32x4 val = o_lds[0][e];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) val += o_lds[w][e];
+            const float L = fin_lds[1][r];
+            val *= L > 0.0f ? 1.0f / L : 0.0f;
+            const float lse = L > 0.0f ? (fin_lds[0][r] + __log2f(L)) * kLn2 : kNegInf;
+            const int rr = it.row0 + r;
+            if (it.part < 0) {
+                const int64_t orow = (int64_t)(si.q_start + rr / G) * a.hq + kvh * G + rr % G;
+                *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.out) + orow * D + d4) =
+                    __builtin_convertvector(val, bf16x4);
+                if (d4 == 0) a.lse[orow] = lse;
+            } else {
+                const int64_t slot_r = it.part + r;
+                *reinterpret_cast<f32x4*>(a.part_o + slot_r * D + d4) = val;
+                if (d4 == 0) a.part_lse[slot_r] = lse;
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -244,9 +407,40 @@ hipError_t launch_unpack4(const Unpack4Args& a, int head_dim, hipStream_t s) {
     return launch(head_dim == 64 ? unpack4_kernel<64> : unpack4_kernel<128>, dim3((unsigned)wgs), dim3(256), a, s);
 }
 
-hipError_t launch_rows4(const KArgs& a, int head_dim, hipStream_t s) {
-    const dim3 g((unsigned)a.n_items * (unsigned)a.hq);
-    return launch(head_dim == 64 ? rows4_kernel<64> : rows4_kernel<128>, g, dim3(256), a, s);
+namespace {
+template <int MODE, int KS64, int KS128>
+hipError_t launch_tile4_mode(const KArgs& a, int head_dim, hipStream_t s) {
+    const dim3 g((unsigned)a.n_wgs);
+    return head_dim == 64 ? launch(tile_kernel<64, 2, kPool4, MODE, 64, KS64>, g, dim3(256 * KS64), a, s)
+                          : launch(tile_kernel<128, 2, kPool4, MODE, 32, KS128>, g, dim3(256 * KS128), a, s);
+}
+}  // namespace
+
+// As launch_tiles, launch_cascade and launch_few for a 16-bit cache.
+hipError_t launch_tiles4(const KArgs& a, int head_dim, hipStream_t s) {
+    if (a.n_items == 0) return hipSuccess;
+    const bool packed = a.group_inv != 0;
+    if (a.key_groups)
+        return packed ? launch_tile4_mode<kPacked, 4, 3>(a, head_dim, s) : launch_tile4_mode<kRows, 4, 3>(a, head_dim, s);
+    return packed ? launch_tile4_mode<kPacked, 1, 1>(a, head_dim, s) : launch_tile4_mode<kRows, 1, 1>(a, head_dim, s);
+}
+
+hipError_t launch_cascade4(const KArgs& a, int head_dim, hipStream_t s) {
+    if (a.n_items == 0) return hipSuccess;
+    return launch_tile4_mode<kCascade, 1, 1>(a, head_dim, s);
+}
+
+hipError_t launch_few4(const KArgs& a, int head_dim, int rb, hipStream_t s) {
+    if (a.n_items == 0) return hipSuccess;
+    const dim3 g(a.n_items), b(256);
+    if (head_dim == 64) {
+        if (rb == 1) return launch(few4_kernel<64, 1>, g, b, a, s);
+        else if (rb == 2) return launch(few4_kernel<64, 2>, g, b, a, s);
+        else return launch(few4_kernel<64, 4>, g, b, a, s);
+    } else {
+        if (rb == 1) return launch(few4_kernel<128, 1>, g, b, a, s);
+        else return launch(few4_kernel<128, 2>, g, b, a, s);
+    }
 }
 
 hipError_t launch_tables(const TablesArgs& a, hipStream_t s) {

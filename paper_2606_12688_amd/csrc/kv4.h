@@ -39,5 +39,30 @@ __device__ __forceinline__ bf16x2 pair_of(uint32_t w, float scale) {
     return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B);
 }
 
+// Four bytes of `w` as eight bf16 values; two from byte B on as four.
+__device__ __forceinline__ bf16x8 eight_of(uint32_t w, float scale) {
+    const bf16x2 a = pair_of<0>(w, scale), b = pair_of<1>(w, scale), c = pair_of<2>(w, scale), d = pair_of<3>(w, scale);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+template <int B>
+__device__ __forceinline__ bf16x4 four_of(uint32_t w, float scale) {
+    const bf16x2 a = pair_of<B>(w, scale), b = pair_of<B + 1>(w, scale);
+    return bf16x4{a[0], a[1], b[0], b[1]};
+}
+
+// Dims 2 b and 2 b + 1 of the D / 16 that a lane's V codes `v` hold of key j.
+template <int D>
+__device__ __forceinline__ bf16x2 v_pair(const uint32_t* v, int j, int b, float scale) {
+    const int byte = D == 128 ? b : 2 * (j & 1) + b;
+    const uint32_t w = v[D == 128 ? j : j >> 1];
+    return byte == 0 ? pair_of<0>(w, scale) : byte == 1 ? pair_of<1>(w, scale) : byte == 2 ? pair_of<2>(w, scale)
+                                                                              : pair_of<3>(w, scale);
+}
+
+// Scale byte j of the four in `w`, at most the largest that a stored row has: a
+// hidden key's probability is 0, and 0 times what any byte up to that one stands
+// for is 0, where an infinity would reach rows that do not see the key.
+__device__ __forceinline__ uint32_t v_scale(uint32_t w, int j) { return min((w >> (8 * j)) & 0xffu, (uint32_t)kScaleMax); }
+
 }  // namespace
 }  // namespace mstar

@@ -1,6 +1,7 @@
-// The multi-row tile kernel.
+// The multi-row tile kernel, over a 16-bit or a 4-bit cache.
 #pragma once
 #include "device.h"
+#include "kv4.h"
 
 namespace mstar {
 namespace {
@@ -44,7 +45,16 @@ constexpr int kTileKeysD128 = MSTAR_TILE_KEYS_D128;
 // pairs of a KV head's group, or entries of a cascade's row list.
 enum { kRows, kPacked, kCascade };
 
-template <int D, int RBW, bool SMALL, int MODE, int BN, int KS>
+// What it reads: a 16-bit pool of up to 2 GB or of any size, or a 4-bit pool.
+//
+// A 4-bit tile cannot go straight into LDS: a wave loads its share (D = 128: the
+// 16 keys of one page, K or V; D = 64: both) into registers a tile ahead, a lane
+// its D / 8 bytes of each record, and converts them into the same LDS image that
+// the direct loads of a 16-bit tile leave, so that each value is converted once
+// per workgroup and everything after it is the same.
+enum { kPoolSmall, kPoolLarge, kPool4 };
+
+template <int D, int RBW, int CACHE, int MODE, int BN, int KS>
 __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void tile_kernel(KArgs a) {
     static_assert(BN == 32 || BN == 64, "tile sizes");
     constexpr int NW = 4;            // waves per key group (32 rows each)
@@ -58,10 +68,12 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     constexpr int RPL = 64 / CH;     // rows filled by one wave-wide load
     constexpr int TB = BN * RBY;     // bytes of one K or V tile
     constexpr int PPT = BN / 16;     // pages per tile
+    constexpr bool SMALL = CACHE == kPoolSmall;
+    static_assert(CACHE != kPool4 || (PPT == NW / 2 && D == 128) || (PPT == NW && D == 64), "shares of a 4-bit tile");
     // two tile buffers per key group ([K, V] of its even and odd tiles): tile
     // t + 1 loads into one while tile t is read from the other
     __shared__ __attribute__((aligned(1024))) char bufs[2][KS][2][TB];
-    __shared__ __attribute__((aligned(256))) int32_t page_rings[KS][2][64];
+    __shared__ __attribute__((aligned(256))) int32_t page_rings[CACHE == kPool4 ? 1 : KS][2][64];
     // each row's visible interval [lo, hi), read on partial tiles only (kept
     // out of the registers the tile loop carries)
     __shared__ __attribute__((aligned(16))) int2 row_lohi[NW][16 * RBW];
@@ -102,7 +114,7 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     const int wave = wave_all & (NW - 1), kg = KS == 1 ? 0 : wave_all / NW;  // wave within its key group, and the group
     char (&buf0)[2][TB] = bufs[0][kg];
     char (&buf1)[2][TB] = bufs[1][kg];
-    int32_t (&page_ring)[2][64] = page_rings[kg];
+    int32_t (&page_ring)[2][64] = page_rings[CACHE == kPool4 ? 0 : kg];
     const int n = lane & 15, grp = lane >> 4;
     const int32_t* bt_row = a.bt + (int64_t)it.seq * a.bt_stride;
     const RowGroup rg;
@@ -342,6 +354,72 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
         }
     };
 
+    // ---- 4-bit loads and conversion ------------------------------------------
+    // wave w's share of a tile: page w % PPT of it, K for the first PPT waves and
+    // V for the others (D = 128), or both (D = 64)
+    typedef Record<D> R;
+    constexpr bool BOTH = PPT == NW;
+    const int share_page = wave % PPT;
+    const bool share_v = wave >= PPT;
+    struct Raw {
+        uint4 code;      // D = 64: K in x and y, V in z and w
+        uint32_t ks, vs;  // K: the scale of this lane's dims of its key; V: those of its four keys, a byte each
+    } raw;
+    // page index of this wave's share of tile tix, read a tile ahead
+    auto share_index = [&](int tix) -> int32_t {
+        const int rel = tix * PPT + share_page;
+        return __builtin_amdgcn_readfirstlane(rel < n_pages ? bt_item[rel] : -1);
+    };
+    int32_t page4 = 0;
+    auto load4 = [&](int tix) {
+        const bool ok = (uint32_t)page4 < (uint32_t)a.num_pages;
+        page_err |= !ok && tix * PPT + share_page < n_pages;
+        const size_t ofs = ok ? ((size_t)page4 * a.hkv + kvh) * R::kBytes : 0;
+        const uint32_t nrec = ok ? (uint32_t)R::kBytes : 0u;  // else reads zeros
+        const uint32_t kscale = R::kScales + (grp * (D / 4) / 32) * 16 + n, vscale = R::scale(4 * grp, n);
+        if constexpr (BOTH) {
+            const __amdgpu_buffer_rsrc_t rk = page_rsrc(kbase, ofs, nrec), rv = page_rsrc(vbase, ofs, nrec);
+            typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+            const u32x2 kc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rk, lane * 8, 0, 0));
+            const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rv, lane * 8, 0, 0));
+            raw.code = uint4{kc[0], kc[1], vc[0], vc[1]};
+            raw.ks = __builtin_amdgcn_raw_buffer_load_b8(rk, (int)kscale, 0, 0);
+            raw.vs = __builtin_amdgcn_raw_buffer_load_b32(rv, (int)vscale, 0, 0);
+        } else {
+            const __amdgpu_buffer_rsrc_t r = page_rsrc(share_v ? vbase : kbase, ofs, nrec);
+            raw.code = load16_at(r, lane * 16);
+            if (share_v) raw.vs = __builtin_amdgcn_raw_buffer_load_b32(r, (int)vscale, 0, 0);
+            else raw.ks = __builtin_amdgcn_raw_buffer_load_b8(r, (int)kscale, 0, 0);
+        }
+        page4 = share_index(tix + 1);
+    };
+    auto store4 = [&](char (&dst)[2][TB]) {
+        if (BOTH || !share_v) {  // K: D / 4 dims of key n, 16-byte chunks in a row
+            const int row = share_page * 16 + n;
+            const float sk = scale_of(raw.ks);
+            const uint32_t w[4] = {raw.code.x, raw.code.y, raw.code.z, raw.code.w};
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+                *reinterpret_cast<bf16x8*>(&dst[0][row * RBY + (((grp * (D / 32) + c) ^ k_swizzle<D>(row)) << 4)]) =
+                    eight_of(w[c], sk);
+        }
+        if (BOTH || share_v) {  // V: D / 16 dims of keys 4 grp .. 4 grp + 3, a piece of each of four rows
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = share_page * 16 + 4 * grp + j;
+                const float sv = scale_of(v_scale(raw.vs, j));
+                if constexpr (D == 128) {
+                    const uint32_t w[4] = {raw.code.x, raw.code.y, raw.code.z, raw.code.w};
+                    *reinterpret_cast<bf16x8*>(&dst[1][row * RBY + ((n ^ v_swizzle<D>(row)) << 4)]) = eight_of(w[j], sv);
+                } else {
+                    const uint32_t w = (j >> 1) ? raw.code.w : raw.code.z;
+                    *reinterpret_cast<bf16x4*>(&dst[1][row * RBY + (((n >> 1) ^ v_swizzle<D>(row)) << 4) + (n & 1) * 8]) =
+                        (j & 1) ? four_of<2>(w, sv) : four_of<0>(w, sv);
+                }
+            }
+        }
+    };
+
     // ---- one tile: scores, mask, online softmax, weighted values ---------------
     const float c2 = a.scale_log2;
     auto scores = [&](const char* kl, f32x4 (&sc)[RBW][NB]) {
@@ -462,7 +540,7 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
         values(vl, pf);
     };
 
-    if (steps > 0) {
+    if (CACHE != kPool4 && steps > 0) {
         load_window(0);
         load_window(1);
         // The Q fragments are consumed here, so the compiler's wait for their
@@ -486,6 +564,31 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
             if (tix + 1 < steps) {
                 dma_barrier();
                 if (tix + 2 < n_tiles) issue_tile(tix + 2, lds_buf0);
+                if (KS == 1 || tix + 1 < n_tiles) compute_tile(tix + 1, buf1);
+            }
+        }
+    }
+    if constexpr (CACHE == kPool4) {
+        // As above, but tile t + 1 goes from registers into the other buffer at
+        // the top of tile t, and the loads of tile t + 2 follow it.
+        if (n_tiles > 0) {
+            page4 = share_index(0);
+            load4(0);
+            store4(buf0);
+            if (n_tiles > 1) load4(1);
+        }
+        auto top = [&](int tix, char (&next)[2][TB]) {
+            lds_barrier();
+            if (tix + 1 < n_tiles) {
+                store4(next);
+                if (tix + 2 < n_tiles) load4(tix + 2);
+            }
+        };
+        for (int tix = 0; tix < steps; tix += 2) {
+            top(tix, buf1);
+            if (KS == 1 || tix < n_tiles) compute_tile(tix, buf0);
+            if (tix + 1 < steps) {
+                top(tix + 1, buf0);
                 if (KS == 1 || tix + 1 < n_tiles) compute_tile(tix + 1, buf1);
             }
         }
