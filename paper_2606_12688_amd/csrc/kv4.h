@@ -50,6 +50,46 @@ __device__ __forceinline__ bf16x4 four_of(uint32_t w, float scale) {
     return bf16x4{a[0], a[1], b[0], b[1]};
 }
 
+// softmax_update with the maximum across a row's four lanes taken only when the
+// reference has to move: a lane compares its own scores with the reference, and
+// none exceeding it by kLazy means that no row's maximum does.  The same results,
+// without the cross-lane exchange in almost every step.
+template <int RB, int NB>
+__device__ __forceinline__ bool softmax_lazy(const RowGroup& rg, f32x4 (&s)[RB][NB], float c, float (&m)[RB],
+                                             float (&l)[RB], float (&alpha)[RB]) {
+    float mx[RB];
+    bool grow = false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        mx[rb] = tree_max<NB>(s[rb]) * c;
+        grow |= mx[rb] > m[rb] + kLazy;
+    }
+    const bool rescale = __builtin_amdgcn_ballot_w64(grow) != 0;
+    float m_use[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        alpha[rb] = 1.0f;
+        if (rescale) {
+            const float m_new = fmax_num(m[rb], rg.max(mx[rb]));
+            alpha[rb] = fast_exp2(m[rb] - (m_new == kNegInf ? 0.0f : m_new));
+            m[rb] = m_new;
+        }
+        m_use[rb] = m[rb] == kNegInf ? 0.0f : m[rb];
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[rb][kb][i] = fast_exp2(fmaf(s[rb][kb][i], c, -m_use[rb]));
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const float sum = tree_sum<NB>(s[rb]);
+        l[rb] = rescale ? l[rb] * alpha[rb] + sum : l[rb] + sum;
+    }
+    return rescale;
+}
+
 // Dims 2 b and 2 b + 1 of the D / 16 that a lane's V codes `v` hold of key j.
 template <int D>
 __device__ __forceinline__ bf16x2 v_pair(const uint32_t* v, int j, int b, float scale) {
