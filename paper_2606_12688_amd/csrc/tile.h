@@ -362,61 +362,71 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     const int share_page = wave % PPT;
     const bool share_v = wave >= PPT;
     struct Raw {
-        uint4 code;      // D = 64: K in x and y, V in z and w
-        uint32_t ks, vs;  // K: the scale of this lane's dims of its key; V: those of its four keys, a byte each
+        uint4 code;           // D = 64: K in x and y, V in z and w
+        uint32_t scale, vs;   // D = 64: of K and of V
     } raw;
-    // page index of this wave's share of tile tix, read a tile ahead
-    auto share_index = [&](int tix) -> int32_t {
-        const int rel = tix * PPT + share_page;
-        return __builtin_amdgcn_readfirstlane(rel < n_pages ? bt_item[rel] : -1);
-    };
-    int32_t page4 = 0;
+    // The item's page indices pass through two registers of 64 (a lane each): a
+    // scalar load in the tile loop would make every wait for LDS reads a wait for
+    // all of them.  Pages past the last one are -1, and no load sits in a branch,
+    // where it could not be counted.
+    auto page_window = [&](int w) { return 64 * w + lane < n_pages ? bt_item[64 * w + lane] : -1; };
+    int32_t pw_cur = -1, pw_next = -1;
     auto load4 = [&](int tix) {
-        const bool ok = (uint32_t)page4 < (uint32_t)a.num_pages;
-        page_err |= !ok && tix * PPT + share_page < n_pages;
-        const size_t ofs = ok ? ((size_t)page4 * a.hkv + kvh) * R::kBytes : 0;
+        const int rel = tix * PPT;
+        if (rel > 0 && (rel & 63) == 0) {
+            pw_cur = pw_next;
+            pw_next = page_window((rel >> 6) + 1);
+        }
+        const int32_t page = __builtin_amdgcn_readlane(pw_cur, (rel & 63) + share_page);
+        const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
+        page_err |= !ok && rel + share_page < n_pages;
+        const size_t ofs = ok ? ((size_t)page * a.hkv + kvh) * R::kBytes : 0;
         const uint32_t nrec = ok ? (uint32_t)R::kBytes : 0u;  // else reads zeros
-        const uint32_t kscale = R::kScales + (grp * (D / 4) / 32) * 16 + n, vscale = R::scale(4 * grp, n);
+        // four scale bytes: K's are those of keys n & ~3 .. n | 3, of which the lane takes its own
+        const uint32_t kscale = R::kScales + (grp * (D / 4) / 32) * 16 + (n & ~3), vscale = R::scale(4 * grp, n);
         if constexpr (BOTH) {
             const __amdgpu_buffer_rsrc_t rk = page_rsrc(kbase, ofs, nrec), rv = page_rsrc(vbase, ofs, nrec);
             typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
             const u32x2 kc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rk, lane * 8, 0, 0));
             const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rv, lane * 8, 0, 0));
             raw.code = uint4{kc[0], kc[1], vc[0], vc[1]};
-            raw.ks = __builtin_amdgcn_raw_buffer_load_b8(rk, (int)kscale, 0, 0);
+            raw.scale = __builtin_amdgcn_raw_buffer_load_b32(rk, (int)kscale, 0, 0);
             raw.vs = __builtin_amdgcn_raw_buffer_load_b32(rv, (int)vscale, 0, 0);
         } else {
             const __amdgpu_buffer_rsrc_t r = page_rsrc(share_v ? vbase : kbase, ofs, nrec);
             raw.code = load16_at(r, lane * 16);
-            if (share_v) raw.vs = __builtin_amdgcn_raw_buffer_load_b32(r, (int)vscale, 0, 0);
-            else raw.ks = __builtin_amdgcn_raw_buffer_load_b8(r, (int)kscale, 0, 0);
+            raw.scale = __builtin_amdgcn_raw_buffer_load_b32(r, (int)(share_v ? vscale : kscale), 0, 0);
         }
-        page4 = share_index(tix + 1);
     };
+    // Where the lane's converted pieces go: the rows and swizzles differ in bits of
+    // their own, so that piece i is at one base with a few bits flipped.
+    //  K: row n of the page, 16-byte chunks D / 32 grp + i;
+    //  V: rows 4 grp + i, D / 16 dims from n D / 16 on.
+    const int k_row = share_page * 16 + n, v_row = share_page * 16 + 4 * grp;
+    const uint32_t k_at = k_row * RBY + (((grp * (D / 32)) ^ k_swizzle<D>(k_row)) << 4);
+    const uint32_t v_at = TB + v_row * RBY + (((n * D / 128) ^ v_swizzle<D>(v_row)) << 4) + (D == 64 ? (n & 1) * 8 : 0);
+    auto v_flip = [](int i) { return D == 128 ? i * 0x120 : i * 0x80 + (i >> 1) * 0x20; };
+    const uint32_t at4 = share_v ? v_at : k_at, flip4 = share_v ? 0x120 : 0x10;
+    // picks the scale of each piece: V's four as they are, K's one for all
+    const uint32_t k_pick = (n & 3) * 0x01010101u, pick4 = share_v ? 0x03020100u : k_pick;
     auto store4 = [&](char (&dst)[2][TB]) {
-        if (BOTH || !share_v) {  // K: D / 4 dims of key n, 16-byte chunks in a row
-            const int row = share_page * 16 + n;
-            const float sk = scale_of(raw.ks);
-            const uint32_t w[4] = {raw.code.x, raw.code.y, raw.code.z, raw.code.w};
+        char* to = &dst[0][0];
+        if constexpr (BOTH) {
+            const float sk = scale_of((raw.scale >> (8 * (n & 3))) & 0xffu);
+            *reinterpret_cast<bf16x8*>(to + k_at) = eight_of(raw.code.x, sk);
+            *reinterpret_cast<bf16x8*>(to + (k_at ^ 0x10)) = eight_of(raw.code.y, sk);
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-                *reinterpret_cast<bf16x8*>(&dst[0][row * RBY + (((grp * (D / 32) + c) ^ k_swizzle<D>(row)) << 4)]) =
-                    eight_of(w[c], sk);
-        }
-        if (BOTH || share_v) {  // V: D / 16 dims of keys 4 grp .. 4 grp + 3, a piece of each of four rows
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = share_page * 16 + 4 * grp + j;
-                const float sv = scale_of(v_scale(raw.vs, j));
-                if constexpr (D == 128) {
-                    const uint32_t w[4] = {raw.code.x, raw.code.y, raw.code.z, raw.code.w};
-                    *reinterpret_cast<bf16x8*>(&dst[1][row * RBY + ((n ^ v_swizzle<D>(row)) << 4)]) = eight_of(w[j], sv);
-                } else {
-                    const uint32_t w = (j >> 1) ? raw.code.w : raw.code.z;
-                    *reinterpret_cast<bf16x4*>(&dst[1][row * RBY + (((n >> 1) ^ v_swizzle<D>(row)) << 4) + (n & 1) * 8]) =
-                        (j & 1) ? four_of<2>(w, sv) : four_of<0>(w, sv);
-                }
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = (i >> 1) ? raw.code.w : raw.code.z;
+                const float sv = scale_of(v_scale(raw.vs, i));
+                *reinterpret_cast<bf16x4*>(to + (v_at ^ v_flip(i))) = (i & 1) ? four_of<2>(w, sv) : four_of<0>(w, sv);
             }
+        } else {
+            const uint32_t w[4] = {raw.code.x, raw.code.y, raw.code.z, raw.code.w};
+            const uint32_t sc = __builtin_amdgcn_perm(raw.scale, raw.scale, pick4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<bf16x8*>(to + (at4 ^ (i * flip4))) = eight_of(w[i], scale_of(v_scale(sc, i)));
         }
     };
 
@@ -571,18 +581,15 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     if constexpr (CACHE == kPool4) {
         // As above, but tile t + 1 goes from registers into the other buffer at
         // the top of tile t, and the loads of tile t + 2 follow it.
-        if (n_tiles > 0) {
-            page4 = share_index(0);
-            load4(0);
-            store4(buf0);
-            if (n_tiles > 1) load4(1);
-        }
+        pw_cur = page_window(0);
+        pw_next = page_window(1);
+        load4(0);
+        store4(buf0);
+        load4(1);
         auto top = [&](int tix, char (&next)[2][TB]) {
             lds_barrier();
-            if (tix + 1 < n_tiles) {
-                store4(next);
-                if (tix + 2 < n_tiles) load4(tix + 2);
-            }
+            store4(next);
+            load4(tix + 2);
         };
         for (int tix = 0; tix < steps; tix += 2) {
             top(tix, buf1);
