@@ -71,83 +71,127 @@ def kv4_pages(num_pages: int, num_kv_heads: int, head_dim: int, device):
     return torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(shape, dtype=torch.uint8, device=device)
 
 
-def _check(tensors, stream):
-    """``(name, tensor, shape, dtype)`` of a call: right shapes and types, dense, and all on the current device.
-    Returns the stream's handle."""
+_torch = None
+_current_device = None  # the current device's index; torch's own function behind torch.cuda.current_device where it is there
+
+
+def _init():
+    global _torch, _current_device
     import torch
 
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    _torch = torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    lib()
+
+
+def _explain(*tensors):
+    """A call that is not in order, taken apart for its message: ``(name, tensor, shape, dtype)`` each."""
+    dev = _torch.cuda.current_device() if _torch.cuda.is_available() else -1
     for name, t, shape, dtype in tensors:
-        if t.get_device() == dev and t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
-            continue
         _need(t.is_cuda and t.get_device() == dev, f"{name} must be on the current device")
         _need(t.dtype == dtype, f"{name} must be {dtype}")
         _need(tuple(t.shape) == tuple(shape), f"{name} must be {list(shape)}")
         _need(t.is_contiguous(), f"{name} must be contiguous")
-    return _stream_handle(stream)
 
 
 def _pool_shape(pl: attn.Plan):
-    p = pl.params
-    return p.num_pages, p.num_kv_heads, record_bytes(p.head_dim)
+    shape = getattr(pl, "_kv4_shape", None)
+    if shape is None:
+        p = pl.params
+        shape = pl._kv4_shape = (p.num_pages, p.num_kv_heads, record_bytes(p.head_dim))
+    return shape
 
 
 def kv4_append(pl: attn.Plan, k_new, v_new, block_table, k_pages, v_pages, stream=None):
     """``mstar_kv4_append`` on torch tensors: round the plan's new K/V rows
     (bf16 ``[total_q, Hkv, d]``, the row numbering of q) to 4 bits and write
     them into their pages of a 4-bit cache."""
-    import torch
+    if _torch is None:
+        _init()
+    pool, dev, bf16, u8, i32 = _pool_shape(pl), k_new.get_device(), _torch.bfloat16, _torch.uint8, _torch.int32
+    if not (dev >= 0 and v_new.get_device() == dev and block_table.get_device() == dev
+            and k_pages.get_device() == dev and v_pages.get_device() == dev and _current_device() == dev
+            and k_new.dtype is bf16 and v_new.dtype is bf16 and block_table.dtype is i32
+            and k_pages.dtype is u8 and v_pages.dtype is u8
+            and k_new.shape == pl._new_shape and v_new.shape == pl._new_shape
+            and block_table.shape == pl._table_shape and k_pages.shape == pool and v_pages.shape == pool
+            and k_new.is_contiguous() and v_new.is_contiguous() and block_table.is_contiguous()
+            and k_pages.is_contiguous() and v_pages.is_contiguous()):
+        _explain(("k_new", k_new, pl._new_shape, bf16), ("v_new", v_new, pl._new_shape, bf16),
+                 ("block_table", block_table, pl._table_shape, i32), ("k_pages", k_pages, pool, u8),
+                 ("v_pages", v_pages, pool, u8))
+    rc = _lib.mstar_kv4_append(pl.handle, k_new.data_ptr(), v_new.data_ptr(), block_table.data_ptr(),
+                               k_pages.data_ptr(), v_pages.data_ptr(), _stream_handle(stream))
+    if rc:
+        _check_rc(rc)
 
-    pool = _pool_shape(pl)
-    s = _check((("k_new", k_new, pl._new_shape, torch.bfloat16), ("v_new", v_new, pl._new_shape, torch.bfloat16),
-                ("block_table", block_table, pl._table_shape, torch.int32),
-                ("k_pages", k_pages, pool, torch.uint8), ("v_pages", v_pages, pool, torch.uint8)), stream)
-    _check_rc(lib().mstar_kv4_append(pl.handle, k_new.data_ptr(), v_new.data_ptr(), block_table.data_ptr(),
-                                     k_pages.data_ptr(), v_pages.data_ptr(), s))
 
-
-def _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse, stream):
-    import torch
-
-    pool = _pool_shape(pl)
-    return _check((("q", q, pl._q_shape, torch.bfloat16), ("k_pages", k_pages, pool, torch.uint8),
-                   ("v_pages", v_pages, pool, torch.uint8),
-                   ("block_table", block_table, pl._table_shape, torch.int32),
-                   ("out", out, pl._q_shape, torch.bfloat16), ("lse", lse, pl._lse_shape, torch.float32)), stream)
+def _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse):
+    if _torch is None:
+        _init()
+    pool, dev, bf16, u8 = _pool_shape(pl), q.get_device(), _torch.bfloat16, _torch.uint8
+    if not (dev >= 0 and k_pages.get_device() == dev and v_pages.get_device() == dev
+            and block_table.get_device() == dev and out.get_device() == dev and lse.get_device() == dev
+            and _current_device() == dev
+            and q.dtype is bf16 and out.dtype is bf16 and k_pages.dtype is u8 and v_pages.dtype is u8
+            and lse.dtype is _torch.float32 and block_table.dtype is _torch.int32
+            and q.shape == pl._q_shape and out.shape == pl._q_shape and lse.shape == pl._lse_shape
+            and k_pages.shape == pool and v_pages.shape == pool and block_table.shape == pl._table_shape
+            and q.is_contiguous() and k_pages.is_contiguous() and v_pages.is_contiguous()
+            and block_table.is_contiguous() and out.is_contiguous() and lse.is_contiguous()):
+        _explain(("q", q, pl._q_shape, bf16), ("k_pages", k_pages, pool, u8), ("v_pages", v_pages, pool, u8),
+                 ("block_table", block_table, pl._table_shape, _torch.int32), ("out", out, pl._q_shape, bf16),
+                 ("lse", lse, pl._lse_shape, _torch.float32))
+    return dev
 
 
 def kv4_fwd(pl: attn.Plan, q, k_pages, v_pages, block_table, out, lse, workspace=None, stream=None):
     """``mstar_kv4_fwd`` on torch tensors: :func:`attn.fwd` over a 4-bit cache.
     ``workspace`` as there (:func:`attn.workspace`)."""
-    s = _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse, stream)
+    dev = _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse)
     ws_ptr, ws_bytes = None, 0
     if workspace is not None:
-        _need(workspace.is_cuda and workspace.device == q.device and workspace.is_contiguous(), "bad workspace")
+        _need(workspace.get_device() == dev and workspace.is_contiguous(), "bad workspace")
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.nbytes
-    _check_rc(lib().mstar_kv4_fwd(pl.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-                                  block_table.data_ptr(), out.data_ptr(), lse.data_ptr(), ws_ptr, ws_bytes, s))
+    rc = _lib.mstar_kv4_fwd(pl.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(),
+                            out.data_ptr(), lse.data_ptr(), ws_ptr, ws_bytes, _stream_handle(stream))
+    if rc:
+        _check_rc(rc)
 
 
 def kv4_fwd_noalloc(pl: attn.Plan, q, k_pages, v_pages, block_table, out, lse, stream=None):
     """``mstar_kv4_fwd_noalloc`` on torch tensors: :func:`attn.fwd_noalloc` over a 4-bit cache."""
-    s = _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse, stream)
-    _check_rc(lib().mstar_kv4_fwd_noalloc(pl.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-                                          block_table.data_ptr(), out.data_ptr(), lse.data_ptr(), s))
+    _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse)
+    rc = _lib.mstar_kv4_fwd_noalloc(pl.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                    block_table.data_ptr(), out.data_ptr(), lse.data_ptr(), _stream_handle(stream))
+    if rc:
+        _check_rc(rc)
 
 
 def kv4_unpack(k_pages, v_pages, page_ids, k_out, v_out, stream=None):
     """``mstar_kv4_unpack`` on torch tensors: pages ``page_ids`` (int32 ``[n]``) of a 4-bit cache as bf16 pages
     ``[n, 16, Hkv, d]``; an index outside the pool gives zeros."""
-    import torch
-
-    _need(k_pages.dim() == 3 and k_out.dim() == 4 and page_ids.dim() == 1, "k_pages, k_out or page_ids has wrong dims")
-    hkv, d = k_pages.shape[1], k_out.shape[3]
-    pool, pages = (k_pages.shape[0], hkv, record_bytes(d)), (page_ids.shape[0], 16, hkv, d)
-    s = _check((("k_pages", k_pages, pool, torch.uint8), ("v_pages", v_pages, pool, torch.uint8),
-                ("page_ids", page_ids, page_ids.shape, torch.int32), ("k_out", k_out, pages, torch.bfloat16),
-                ("v_out", v_out, pages, torch.bfloat16)), stream)
-    _check_rc(lib().mstar_kv4_unpack(hkv, d, k_pages.shape[0], k_pages.data_ptr(), v_pages.data_ptr(),
-                                     page_ids.data_ptr(), page_ids.shape[0], k_out.data_ptr(), v_out.data_ptr(), s))
+    if _torch is None:
+        _init()
+    shape, pages = k_pages.shape, k_out.shape
+    _need(len(shape) == 3 and len(pages) == 4 and page_ids.dim() == 1, "k_pages, k_out or page_ids has wrong dims")
+    (num_pages, hkv, record), n, d = shape, page_ids.shape[0], pages[3]
+    dev, bf16, u8 = k_pages.get_device(), _torch.bfloat16, _torch.uint8
+    if not (dev >= 0 and v_pages.get_device() == dev and page_ids.get_device() == dev and k_out.get_device() == dev
+            and v_out.get_device() == dev and _current_device() == dev
+            and k_pages.dtype is u8 and v_pages.dtype is u8 and page_ids.dtype is _torch.int32
+            and k_out.dtype is bf16 and v_out.dtype is bf16
+            and record == record_bytes(d) and v_pages.shape == shape and pages == (n, 16, hkv, d)
+            and v_out.shape == pages
+            and k_pages.is_contiguous() and v_pages.is_contiguous() and page_ids.is_contiguous()
+            and k_out.is_contiguous() and v_out.is_contiguous()):
+        pool, out = (num_pages, hkv, record_bytes(d)), (n, 16, hkv, d)
+        _explain(("k_pages", k_pages, pool, u8), ("v_pages", v_pages, pool, u8),
+                 ("page_ids", page_ids, (n,), _torch.int32), ("k_out", k_out, out, bf16), ("v_out", v_out, out, bf16))
+    rc = _lib.mstar_kv4_unpack(hkv, d, num_pages, k_pages.data_ptr(), v_pages.data_ptr(), page_ids.data_ptr(), n,
+                               k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
+    if rc:
+        _check_rc(rc)
 
 
 def block_tables_pages(pl: attn.Plan) -> int:
@@ -155,20 +199,28 @@ def block_tables_pages(pl: attn.Plan) -> int:
     return int(lib().mstar_block_tables_pages(pl.handle))
 
 
-def block_tables(pl: attn.Plan, free_pages, block_table, slots=None, stream=None) -> int:
+def block_tables(pl: attn.Plan, free_pages, block_table, slots=None, stream=None):
     """``mstar_block_tables`` on torch tensors: the pages of the plan's new rows,
-    taken from the front of ``free_pages`` (int32 ``[m]``), are entered into
-    ``block_table`` (int32 ``[num_seqs, max_blocks]``), and ``slots`` (int64
-    ``[total_q]``, optional) gets every new row's flat slot.  Returns the number
-    of pages taken."""
-    import torch
-
-    _need(free_pages.dim() == 1, "free_pages must have one dimension")
-    tensors = [("free_pages", free_pages, free_pages.shape, torch.int32),
-               ("block_table", block_table, pl._table_shape, torch.int32)]
+    taken from the front of ``free_pages`` (int32 ``[m]``; :func:`block_tables_pages`
+    says how many), are entered into ``block_table`` (int32 ``[num_seqs,
+    max_blocks]``), and ``slots`` (int64 ``[total_q]``, optional) gets every new
+    row's flat slot."""
+    if _torch is None:
+        _init()
+    dev, i32 = block_table.get_device(), _torch.int32
+    if not (dev >= 0 and free_pages.get_device() == dev and _current_device() == dev
+            and free_pages.dtype is i32 and block_table.dtype is i32
+            and free_pages.dim() == 1 and block_table.shape == pl._table_shape
+            and free_pages.is_contiguous() and block_table.is_contiguous()):
+        _explain(("free_pages", free_pages, (free_pages.numel(),), i32),
+                 ("block_table", block_table, pl._table_shape, i32))
+    slots_ptr = None
     if slots is not None:
-        tensors.append(("slots", slots, (pl.total_q,), torch.int64))
-    s = _check(tensors, stream)
-    _check_rc(lib().mstar_block_tables(pl.handle, free_pages.data_ptr(), free_pages.shape[0],
-                                       block_table.data_ptr(), None if slots is None else slots.data_ptr(), s))
-    return block_tables_pages(pl)
+        if not (slots.get_device() == dev and slots.dtype is _torch.int64 and slots.shape == (pl.total_q,)
+                and slots.is_contiguous()):
+            _explain(("slots", slots, (pl.total_q,), _torch.int64))
+        slots_ptr = slots.data_ptr()
+    rc = _lib.mstar_block_tables(pl.handle, free_pages.data_ptr(), free_pages.shape[0], block_table.data_ptr(),
+                                 slots_ptr, _stream_handle(stream))
+    if rc:
+        _check_rc(rc)

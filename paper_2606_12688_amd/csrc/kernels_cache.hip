@@ -7,70 +7,126 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // Append: a workgroup takes up to 16 new rows of one request, a wave one KV head
-// of the rows of one aligned group of four positions at a time: lane 4 n + j holds
-// dims [n D / 16, +D / 16) of the group's key j, so that its V words are
-// consecutive and its K words run over 64 (D = 128) or 32 bytes of each piece.
-// The 32 dims of a scale are 4 (D = 128) or 8 neighbouring n.
+// of them at a time, by aligned groups of four positions (at most five): lane
+// 4 n + j holds dims [n D / 16, +D / 16) of a group's key j, so that its V words
+// are consecutive and its K words run over 64 (D = 128) or 32 bytes of each
+// piece.  The 32 dims of a scale are 4 (D = 128) or 8 neighbouring n.
 // ---------------------------------------------------------------------------
+// A lane's D / 16 bf16 values as packed pairs.
+template <int D>
+struct Piece {
+    uint32_t w[D / 32];
+};
+template <int D>
+__device__ __forceinline__ Piece<D> load_piece(const void* rows, int64_t elem) {
+    Piece<D> p;
+    if constexpr (D == 128) {
+        const uint4 u = load16(rows, elem);
+        p.w[0] = u.x; p.w[1] = u.y; p.w[2] = u.z; p.w[3] = u.w;
+    } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(rows) + elem);
+        p.w[0] = u.x; p.w[1] = u.y;
+    }
+    return p;
+}
+
+// Codes (one byte per pair) and scale byte of a lane's piece, whose block's other
+// dims are with the lanes that differ in bits 2, 3 (and 4 at D = 64).  The scale
+// is exact; the conversion divides by it and rounds once, to the nearest code,
+// ties to even.  `odd` tells of an infinity or a NaN; NaN becomes 0.
+template <int D>
+__device__ __forceinline__ uint32_t round_piece(Piece<D>& p, int& b, bool& odd) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top2 = {0, 0};
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+        top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, p.w[i] & 0x7fff7fffu));
+    uint32_t top = max((uint32_t)top2[0], (uint32_t)top2[1]);
+    if (top >= 0x7f80u) {
+        odd = true;
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            uint32_t lo = p.w[i] & 0xffffu, hi = p.w[i] >> 16;
+            if ((lo & 0x7fffu) > 0x7f80u) lo = 0;
+            if ((hi & 0x7fffu) > 0x7f80u) hi = 0;
+            p.w[i] = lo | (hi << 16);
+            top = max(top, max(lo & 0x7fffu, hi & 0x7fffu));
+        }
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 4, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 8, 64));
+    if (D == 64) top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+    // smallest b with top <= 7 * 2^(b - 127): 7 is mantissa 0x60 two binades up
+    b = min(max((int)((top + 31) >> 7) - 2, kScaleMin), kScaleMax);
+    const float s = scale_of((uint32_t)b);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, p.w[0]), s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, p.w[1]), s, 1);
+    if constexpr (D == 128) {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, p.w[2]), s, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, p.w[3]), s, 3);
+    }
+    return c;
+}
+
 template <int D>
 __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
-    constexpr int E = D / 16;  // dims per lane
+    constexpr int E = D / 16;        // dims per lane
+    constexpr int GR = kAppendRows / 4 + 1;  // groups of four positions that 16 rows touch
     typedef Record<D> R;
     const WorkItem it = a.items[wg_id()];
     const SeqInfo si = a.seqs[it.seq];
     const int wave = __builtin_amdgcn_readfirstlane(thread_id() >> 6) & 3, lane = thread_id() & 63;
     const int n = lane >> 2, j = lane & 3;
     const int32_t* bt_row = a.bt + (int64_t)it.seq * a.bt_stride;
-    const int32_t g0 = it.k_begin >> 2, groups = ((it.k_end - 1) >> 2) - g0 + 1;
-    bool bad_page = false, bad_value = false;
-    for (int t = wave; t < groups * a.hkv; t += 4) {
-        const int g = t / a.hkv, head = t - g * a.hkv;
-        const int32_t pos = 4 * (g0 + g) + j, slot = pos & 15;
-        bool live = pos >= it.k_begin && pos < it.k_end;
-        const int32_t page = live ? bt_row[pos >> 4] : 0;
-        if ((uint32_t)page >= (uint32_t)a.num_pages) {
-            bad_page = true;
-            live = false;
+    const int32_t p0 = it.k_begin & ~3;
+    bool live[GR], bad_page = false, bad_value = false;
+    int32_t page[GR];
+#pragma unroll
+    for (int g = 0; g < GR; ++g) {
+        const int32_t pos = p0 + 4 * g + j;
+        live[g] = pos >= it.k_begin && pos < it.k_end;
+        page[g] = live[g] ? bt_row[pos >> 4] : 0;
+    }
+    const int64_t row0 = si.q_start + (p0 + j - (si.kv_len - si.q_len));
+    for (int head = wave; head < a.hkv; head += 4) {
+        // every row's loads before any is used, and before the page indices are
+        Piece<D> k[GR], v[GR];
+#pragma unroll
+        for (int g = 0; g < GR; ++g) {
+            k[g] = v[g] = Piece<D>{};
+            if (live[g]) {
+                const int64_t src = ((row0 + 4 * g) * a.hkv + head) * D + n * E;
+                k[g] = load_piece<D>(a.k_new, src);
+                v[g] = load_piece<D>(a.v_new, src);
+            }
         }
-        const int64_t row = si.q_start + (pos - (si.kv_len - si.q_len));
-        const int64_t src = (row * a.hkv + head) * D + n * E;
-        const int64_t rec = ((int64_t)page * a.hkv + head) * R::kBytes;
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {  // K, V
-            uint32_t x[E];
-            const uint16_t* in = reinterpret_cast<const uint16_t*>(m == 0 ? a.k_new : a.v_new) + src;
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                x[e] = live ? in[e] : 0;
-                bad_value |= (x[e] & 0x7fff) >= 0x7f80;
-                if ((x[e] & 0x7fff) > 0x7f80) x[e] = 0;
-                top = max(top, x[e] & 0x7fff);
+        for (int g = 0; g < GR; ++g) {
+            if (p0 + 4 * g >= it.k_end) continue;
+            int kb, vb;
+            const uint32_t kw = round_piece<D>(k[g], kb, bad_value), vw = round_piece<D>(v[g], vb, bad_value);
+            if (!live[g]) continue;
+            if ((uint32_t)page[g] >= (uint32_t)a.num_pages) {
+                bad_page = true;
+                continue;
             }
-            // the largest magnitude of the scale's 32 dims
-            top = max(top, (uint32_t)__shfl_xor((int)top, 4, 64));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 8, 64));
-            if (D == 64) top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-            // smallest b with top <= 7 * 2^(b - 127): 7 is mantissa 0x60 two binades up
-            const int b = min(max((int)((top + 31) >> 7) - 2, kScaleMin), kScaleMax);
-            const float inv = __uint_as_float((uint32_t)(254 - b) << 23);  // exact
-            uint32_t w = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float y = __uint_as_float((x[e] & 0x7fff) << 16) * inv;
-                // nearest of 0, .5, 1, 1.5, 2, 3, 4, 6, ties to the even code
-                const uint32_t c = (y > 0.25f) + (y >= 0.75f) + (y > 1.25f) + (y >= 1.75f) + (y > 2.5f) +
-                                   (y >= 3.5f) + (y > 5.0f);
-                w |= (c | (x[e] >> 15) << 3) << (4 * e);
+            const int slot = (p0 + 4 * g + j) & 15;
+            const int64_t rec = ((int64_t)page[g] * a.hkv + head) * R::kBytes;
+            char* kr = static_cast<char*>(a.k) + rec;
+            char* vr = static_cast<char*>(a.v) + rec;
+            if constexpr (D == 128) {
+                *reinterpret_cast<uint32_t*>(kr + R::k_word(slot, n)) = kw;
+                *reinterpret_cast<uint32_t*>(vr + R::v_word(slot, n)) = vw;
+            } else {
+                *reinterpret_cast<uint16_t*>(kr + R::k_word(slot, n)) = (uint16_t)kw;
+                *reinterpret_cast<uint16_t*>(vr + R::v_word(slot, n)) = (uint16_t)vw;
             }
-            if (!live) continue;
-            char* to = static_cast<char*>(m == 0 ? a.k : a.v) + rec;
-            char* word = to + (m == 0 ? R::k_word(slot, n) : R::v_word(slot, n));
-            if (D == 128)
-                *reinterpret_cast<uint32_t*>(word) = w;
-            else
-                *reinterpret_cast<uint16_t*>(word) = (uint16_t)w;
-            if (n % (32 / E) == 0) to[R::scale(slot, n)] = (char)b;
+            if (n % (32 / E) == 0) {
+                kr[R::scale(slot, n)] = (char)kb;
+                vr[R::scale(slot, n)] = (char)vb;
+            }
         }
     }
     const int bits = (__builtin_amdgcn_ballot_w64(bad_page) ? MSTAR_DEVERR_PAGE_RANGE_BIT : 0) |

@@ -363,7 +363,7 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     const bool share_v = wave >= PPT;
     struct Raw {
         uint4 code;           // D = 64: K in x and y, V in z and w
-        uint32_t scale, vs;   // D = 64: of K and of V
+        uint32_t scale, vs;   // D = 64: of K (one byte) and of V
     } raw;
     // The item's page indices pass through two registers of 64 (a lane each): a
     // scalar load in the tile loop would make every wait for LDS reads a wait for
@@ -382,15 +382,16 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
         page_err |= !ok && rel + share_page < n_pages;
         const size_t ofs = ok ? ((size_t)page * a.hkv + kvh) * R::kBytes : 0;
         const uint32_t nrec = ok ? (uint32_t)R::kBytes : 0u;  // else reads zeros
-        // four scale bytes: K's are those of keys n & ~3 .. n | 3, of which the lane takes its own
-        const uint32_t kscale = R::kScales + (grp * (D / 4) / 32) * 16 + (n & ~3), vscale = R::scale(4 * grp, n);
+        // four scale bytes of V; of K the one byte (D = 64), or those of keys n & ~3 .. n | 3
+        const uint32_t kscale = R::kScales + (grp * (D / 4) / 32) * 16 + (BOTH ? n : n & ~3);
+        const uint32_t vscale = R::scale(4 * grp, n);
         if constexpr (BOTH) {
             const __amdgpu_buffer_rsrc_t rk = page_rsrc(kbase, ofs, nrec), rv = page_rsrc(vbase, ofs, nrec);
             typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
             const u32x2 kc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rk, lane * 8, 0, 0));
             const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rv, lane * 8, 0, 0));
             raw.code = uint4{kc[0], kc[1], vc[0], vc[1]};
-            raw.scale = __builtin_amdgcn_raw_buffer_load_b32(rk, (int)kscale, 0, 0);
+            raw.scale = __builtin_amdgcn_raw_buffer_load_b8(rk, (int)kscale, 0, 0);
             raw.vs = __builtin_amdgcn_raw_buffer_load_b32(rv, (int)vscale, 0, 0);
         } else {
             const __amdgpu_buffer_rsrc_t r = page_rsrc(share_v ? vbase : kbase, ofs, nrec);
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     auto store4 = [&](char (&dst)[2][TB]) {
         char* to = &dst[0][0];
         if constexpr (BOTH) {
-            const float sk = scale_of((raw.scale >> (8 * (n & 3))) & 0xffu);
+            const float sk = scale_of(raw.scale);
             *reinterpret_cast<bf16x8*>(to + k_at) = eight_of(raw.code.x, sk);
             *reinterpret_cast<bf16x8*>(to + (k_at ^ 0x10)) = eight_of(raw.code.y, sk);
 #pragma unroll
