@@ -67,7 +67,8 @@ int mstar_kv4_fwd(const mstar_plan_t* plan, const void* q, const void* k_pages, 
                   hipStream_t stream);
 
 /* mstar_attn_fwd_noalloc over a 4-bit cache: the partials go to the library's
- * static device array, which all such calls on a GPU share. */
+ * static device array, which all such calls on a GPU (and those of
+ * mstar_attn_fwd_noalloc) share, so that no two of them may overlap in time. */
 int mstar_kv4_fwd_noalloc(const mstar_plan_t* plan, const void* q, const void* k_pages, const void* v_pages,
                           const int32_t* block_table, void* out, float* lse, hipStream_t stream);
 

@@ -26,6 +26,7 @@ struct Unpack4Args {
     void* k_out;    // [n_ids][16][hkv][head_dim] bf16
     void* v_out;
     int32_t n_ids, hkv, num_pages;
+    int32_t n_wgs;    // set by the launch
     hipEvent_t done;  // NULL
 };
 

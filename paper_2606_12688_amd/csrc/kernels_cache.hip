@@ -1,5 +1,7 @@
 // HIP kernels of the operators on paged caches (mstar_cache.h) for gfx950: the
 // 4-bit cache's append, attention and read-back, and block tables.
+#include <algorithm>
+
 #include "tile.h"
 
 namespace mstar {
@@ -21,11 +23,12 @@ template <int D>
 __device__ __forceinline__ Piece<D> load_piece(const void* rows, int64_t elem) {
     Piece<D> p;
     if constexpr (D == 128) {
-        const uint4 u = load16(rows, elem);
+        const uint4 u = load16_nt(rows, elem);
         p.w[0] = u.x; p.w[1] = u.y; p.w[2] = u.z; p.w[3] = u.w;
     } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(rows) + elem);
-        p.w[0] = u.x; p.w[1] = u.y;
+        typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 u = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const bf16_t*>(rows) + elem));
+        p.w[0] = u[0]; p.w[1] = u[1];
     }
     return p;
 }
@@ -137,16 +140,19 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
 // ---------------------------------------------------------------------------
 // Unpack: a wave takes one record of a listed page, four keys at a time; lane
 // 16 g + n writes dims [n D / 16, +D / 16) of the group's key g.
+//
+// Bound: HBM, mostly the pages written.  Rows that the append reads and pages that
+// this writes are non-temporal: 34816 rows of 4 heads stored and read back (D =
+// 128, 180 MB) 48 -> 39 us.
 // ---------------------------------------------------------------------------
 template <int D>
 __device__ __forceinline__ void store_word(bf16_t* out, uint32_t w, float s) {
-    const bf16x2 p0 = pair_of<0>(w, s), p1 = pair_of<1>(w, s);
-    if constexpr (D == 128) {
-        const bf16x2 p2 = pair_of<2>(w, s), p3 = pair_of<3>(w, s);
-        *reinterpret_cast<bf16x8*>(out) = bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-    } else {
-        *reinterpret_cast<bf16x4*>(out) = bf16x4{p0[0], p0[1], p1[0], p1[1]};
-    }
+    typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+    typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+    if constexpr (D == 128)
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, eight_of(w, s)), reinterpret_cast<u32x4*>(out));
+    else
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x2, four_of<0>(w, s)), reinterpret_cast<u32x2*>(out));
 }
 
 template <int D>
@@ -154,27 +160,28 @@ __global__ __launch_bounds__(256) void unpack4_kernel(Unpack4Args a) {
     typedef Record<D> R;
     const int wave = __builtin_amdgcn_readfirstlane(thread_id() >> 6) & 3, lane = thread_id() & 63;
     const int g = lane >> 4, n = lane & 15;
-    const int64_t task = (int64_t)wg_id() * 4 + wave;
-    if (task >= (int64_t)a.n_ids * a.hkv) return;
-    const int64_t i = task / a.hkv;
-    const int head = (int)(task - i * a.hkv);
-    const int32_t page = a.ids[i];
-    const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
-    const int64_t rec = ok ? ((int64_t)page * a.hkv + head) * R::kBytes : 0;
+    const int64_t tasks = (int64_t)a.n_ids * a.hkv;
+    for (int64_t task = (int64_t)wg_id() * 4 + wave; task < tasks; task += 4 * (int64_t)a.n_wgs) {
+        const int64_t i = task / a.hkv;
+        const int head = (int)(task - i * a.hkv);
+        const int32_t page = a.ids[i];
+        const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
+        const int64_t rec = ok ? ((int64_t)page * a.hkv + head) * R::kBytes : 0;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-        const unsigned char* from = static_cast<const unsigned char*>(m == 0 ? a.k : a.v) + rec;
-        bf16_t* out = static_cast<bf16_t*>(m == 0 ? a.k_out : a.v_out);
+        for (int m = 0; m < 2; ++m) {
+            const unsigned char* from = static_cast<const unsigned char*>(m == 0 ? a.k : a.v) + rec;
+            bf16_t* out = static_cast<bf16_t*>(m == 0 ? a.k_out : a.v_out);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int slot = 4 * c + g;
-            uint32_t w = 0, b = 0;
-            if (ok) {
-                const unsigned char* word = from + (m == 0 ? R::k_word(slot, n) : R::v_word(slot, n));
-                w = D == 128 ? *reinterpret_cast<const uint32_t*>(word) : *reinterpret_cast<const uint16_t*>(word);
-                b = from[R::scale(slot, n)];
+            for (int c = 0; c < 4; ++c) {
+                const int slot = 4 * c + g;
+                uint32_t w = 0, b = 0;
+                if (ok) {
+                    const unsigned char* word = from + (m == 0 ? R::k_word(slot, n) : R::v_word(slot, n));
+                    w = D == 128 ? *reinterpret_cast<const uint32_t*>(word) : *reinterpret_cast<const uint16_t*>(word);
+                    b = from[R::scale(slot, n)];
+                }
+                store_word<D>(out + ((i * 16 + slot) * a.hkv + head) * D + n * (D / 16), w, scale_of(b));
             }
-            store_word<D>(out + ((i * 16 + slot) * a.hkv + head) * D + n * (D / 16), w, scale_of(b));
         }
     }
 }
@@ -492,9 +499,10 @@ hipError_t launch_append4(const Append4Args& a, int head_dim, hipStream_t s) {
 }
 
 hipError_t launch_unpack4(const Unpack4Args& a, int head_dim, hipStream_t s) {
-    const int64_t wgs = ((int64_t)a.n_ids * a.hkv + 3) / 4;
-    if (wgs > INT32_MAX) return hipErrorInvalidValue;
-    return launch(head_dim == 64 ? unpack4_kernel<64> : unpack4_kernel<128>, dim3((unsigned)wgs), dim3(256), a, s);
+    // a wave per record, in several turns past 2^20 workgroups
+    Unpack4Args b = a;
+    b.n_wgs = (int32_t)std::min<int64_t>(((int64_t)a.n_ids * a.hkv + 3) / 4, 1 << 20);
+    return launch(head_dim == 64 ? unpack4_kernel<64> : unpack4_kernel<128>, dim3(b.n_wgs), dim3(256), b, s);
 }
 
 namespace {

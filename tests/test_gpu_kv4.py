@@ -484,3 +484,22 @@ def test_rounding_matches_the_oracle_over_every_bf16_value():
         page, slot = b.block_table[0, rows // 16], rows % 16
         assert np.array_equal(s[page, slot], scales), which
         assert np.array_equal(c[page, slot], codes), which
+
+
+def test_unpack_of_more_records_than_one_launch_has_waves():
+    import torch
+
+    n = (1 << 22) + 5
+    rng = np.random.default_rng(3)
+    pools = rng.integers(0, 256, (2, 7, 1, 544)).astype(np.uint8)
+    pools[..., 512:] = rng.integers(100, 140, pools[..., 512:].shape)
+    k4, v4 = (torch.from_numpy(p).to(DEV) for p in pools)
+    ids = torch.arange(n, dtype=torch.int32, device=DEV) % 8  # 7 is outside the pool
+    out = [torch.empty((n, 16, 1, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    cache.kv4_unpack(k4, v4, ids, *out)
+    for which, p, got in zip("kv", pools, out):
+        want = np.concatenate([kv4_values(*kv4_read(which, p, 64)), np.zeros((1, 16, 1, 64))])
+        want = torch.from_numpy(want).to(DEV).bfloat16()
+        whole = n // 8 * 8
+        assert (got[:whole].view(-1, 8, 16, 1, 64) == want).all()
+        assert torch.equal(got[whole:], want[:n - whole])
