@@ -347,16 +347,21 @@ int mstar::run_fwd(const Launchers& kernels, const mstar_plan* plan, const void*
     hipError_t e;
     hipEvent_t use = nullptr;
     if ((e = use_event(plan, s, &use)) != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
+    // few-row items that go with the tiles', or else the cascade's, launch
+    const bool mix = kernels.mixed && !h.few.empty() && h.decode_rb <= 2 && !(h.params.flags & MSTAR_FLAG_SERIAL);
+    const bool with_tiles = mix && !h.tiles.empty() && !h.key_groups;
+    const bool with_cascade = mix && h.tiles.empty() && !h.cascade.empty();
+    const bool forked = plan->forked && !with_tiles;
     // the kernel class that ends the call carries the use event (none does
     // when the call ends with the wait for the side stream)
-    const int last = !h.merges.empty() ? 3 : plan->forked ? -1 : !h.f32.empty() ? 2 : !h.cascade.empty() ? 4 : !h.tiles.empty() ? 0 : 1;
+    const int last = !h.merges.empty() ? 3 : forked ? -1 : !h.f32.empty() ? 2 : !h.cascade.empty() ? 4 : !h.tiles.empty() ? 0 : 1;
     auto done = [&](int k) { return k == last ? use : nullptr; };
     // The few-row kernel runs on the thread's side stream when the plan also
     // has tile work: it streams K/V from HBM while the tile kernel keeps the
     // matrix units busy.  Both write disjoint outputs and partial slots; the
     // merge waits for both.
     PlanBlock* b = plan->blk;
-    hipStream_t side = plan->forked ? b->side : nullptr;
+    hipStream_t side = forked ? b->side : nullptr;
     if (side) {
         if ((e = hipEventRecord(b->fork, s)) != hipSuccess) return hip_fail(e, "hipEventRecord(fork)");
         if ((e = hipStreamWaitEvent(side, b->fork, 0)) != hipSuccess) return hip_fail(e, "hipStreamWaitEvent(fork)");
@@ -370,12 +375,13 @@ int mstar::run_fwd(const Launchers& kernels, const mstar_plan* plan, const void*
     };
 #define MSTAR_MARK(evs, k) \
     if ((e = mark(evs, k)) != hipSuccess) return hip_fail(e, "hipEventRecord")
-    if (!h.few.empty()) {
-        a.items = reinterpret_cast<const mstar::WorkItem*>(blob + plan->off_few);
-        a.n_items = (int32_t)h.few.size();
-        a.done = done(1);
+    mstar::KArgs few = a;
+    few.items = reinterpret_cast<const mstar::WorkItem*>(blob + plan->off_few);
+    few.n_items = (int32_t)h.few.size();
+    if (!h.few.empty() && !with_tiles && !with_cascade) {
+        few.done = done(1);
         MSTAR_MARK(events_before, 1);
-        if ((e = kernels.few(a, D, h.decode_rb, s_few)) != hipSuccess) return hip_fail(e, "few-row kernel launch");
+        if ((e = kernels.few(few, D, h.decode_rb, s_few)) != hipSuccess) return hip_fail(e, "few-row kernel launch");
         MSTAR_MARK(events_after, 1);
     }
     if (side) {
@@ -390,7 +396,8 @@ int mstar::run_fwd(const Launchers& kernels, const mstar_plan* plan, const void*
         a.span_step = std::max(512, h.tile_span / 4);
         a.done = done(0);
         MSTAR_MARK(events_before, 0);
-        if ((e = kernels.tiles(a, D, s)) != hipSuccess) return hip_fail(e, "tile kernel launch");
+        e = with_tiles ? kernels.mixed(a, few, false, D, h.decode_rb, s) : kernels.tiles(a, D, s);
+        if (e != hipSuccess) return hip_fail(e, "tile kernel launch");
         MSTAR_MARK(events_after, 0);
     }
     if (!h.cascade.empty()) {
@@ -403,7 +410,8 @@ int mstar::run_fwd(const Launchers& kernels, const mstar_plan* plan, const void*
         a.rows = reinterpret_cast<const int32_t*>(blob + plan->off_casc_rows);
         a.done = done(4);
         MSTAR_MARK(events_before, 4);
-        if ((e = kernels.cascade(a, D, s)) != hipSuccess) return hip_fail(e, "cascade kernel launch");
+        e = with_cascade ? kernels.mixed(a, few, true, D, h.decode_rb, s) : kernels.cascade(a, D, s);
+        if (e != hipSuccess) return hip_fail(e, "cascade kernel launch");
         MSTAR_MARK(events_after, 4);
     }
     if (side) {
@@ -459,7 +467,7 @@ int mstar::run_fwd_noalloc(const Launchers& kernels, const mstar_plan* plan, con
 }
 
 namespace {
-constexpr mstar::Launchers kKernels = {mstar::launch_tiles, mstar::launch_few, mstar::launch_cascade};
+constexpr mstar::Launchers kKernels = {mstar::launch_tiles, mstar::launch_few, mstar::launch_cascade, nullptr};
 }
 
 MSTAR_EXPORT int mstar_attn_fwd(const mstar_plan_t* plan, const void* q, const void* k_pages,

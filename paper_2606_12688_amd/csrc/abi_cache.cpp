@@ -31,7 +31,8 @@ int check_plan4(const mstar_plan* plan) {
     return MSTAR_OK;
 }
 
-constexpr mstar::Launchers kKernels4 = {mstar::launch_tiles4, mstar::launch_few4, mstar::launch_cascade4};
+constexpr mstar::Launchers kKernels4 = {mstar::launch_tiles4, mstar::launch_few4, mstar::launch_cascade4,
+                                        mstar::launch_mixed4};
 
 template <typename T>
 T* at(const mstar_plan* plan, size_t off) {

@@ -49,6 +49,9 @@ hipError_t launch_tables(const TablesArgs& a, hipStream_t s);
 // Attention over a 4-bit cache: k and v of KArgs are 4-bit pools.
 hipError_t launch_tiles4(const KArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_cascade4(const KArgs& a, int head_dim, hipStream_t s);
+// Multi-row (or cascade) work and few-row items of one or two row blocks in one
+// launch; tile.done goes with it.
+hipError_t launch_mixed4(const KArgs& tile, const KArgs& few, bool cascade, int head_dim, int row_blocks, hipStream_t s);
 hipError_t launch_few4(const KArgs& a, int head_dim, int row_blocks, hipStream_t s);
 
 }  // namespace mstar

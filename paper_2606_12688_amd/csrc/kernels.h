@@ -34,6 +34,12 @@ struct KArgs {
     hipEvent_t done;  // host side: NULL, or an event that completes with the kernel (not under capture)
 };
 
+// A launch that holds both multi-row work and few-row items (4-bit cache only).
+struct MixedArgs {
+    KArgs tile, few;  // the tiles' workgroups first
+    hipEvent_t done;  // host side: NULL, or an event that completes with the kernel (not under capture)
+};
+
 struct MArgs {
     const MergeItem* items;
     const float* part_o;

@@ -68,6 +68,8 @@ struct Launchers {
     hipError_t (*tiles)(const KArgs& a, int head_dim, hipStream_t s);
     hipError_t (*few)(const KArgs& a, int head_dim, int row_blocks, hipStream_t s);
     hipError_t (*cascade)(const KArgs& a, int head_dim, hipStream_t s);
+    // NULL, or one launch for multi-row (or cascade) work and few-row items of one or two row blocks
+    hipError_t (*mixed)(const KArgs& tile, const KArgs& few, bool cascade, int head_dim, int row_blocks, hipStream_t s);
 };
 
 // Checks the arguments and enqueues the plan's kernels (see mstar_attn_fwd_timed).

@@ -1,7 +1,9 @@
 // The multi-row tile kernel, over a 16-bit or a 4-bit cache.
 #pragma once
+#include <type_traits>
+
 #include "device.h"
-#include "kv4.h"
+#include "few4.h"
 
 namespace mstar {
 namespace {
@@ -54,8 +56,21 @@ enum { kRows, kPacked, kCascade };
 // per workgroup and everything after it is the same.
 enum { kPoolSmall, kPoolLarge, kPool4 };
 
-template <int D, int RBW, int CACHE, int MODE, int BN, int KS>
-__global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void tile_kernel(KArgs a) {
+// FEW > 0: the launch also holds the few-row items of a 4-bit cache, of FEW 16-row
+// blocks, in workgroups of their own behind the tiles': they stream from memory
+// while the last tiles keep the matrix units busy, without a side stream's fork
+// and join, at the tiles' occupancy.  128 decode steps behind a shared prefix 42.5
+// -> 34 us; 48 decode steps beside a prompt of 1000 tokens 52 -> 44, beside 64
+// chunks and an image of 4352 319 -> 310; 96 beside four prompts of 2500 and the
+// image 520 -> 491.  Spread evenly among the tiles instead, they took up to 50%
+// longer (a prompt's last tiles start late).
+__device__ __forceinline__ const KArgs& tile_args(const KArgs& a) { return a; }
+__device__ __forceinline__ const KArgs& tile_args(const MixedArgs& a) { return a.tile; }
+
+template <int D, int RBW, int CACHE, int MODE, int BN, int KS, int FEW = 0>
+__global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void tile_kernel(
+    std::conditional_t<FEW == 0, KArgs, MixedArgs> args) {
+    const KArgs& a = tile_args(args);
     static_assert(BN == 32 || BN == 64, "tile sizes");
     constexpr int NW = 4;            // waves per key group (32 rows each)
     constexpr int NB = BN / 16;      // 16-key blocks of a tile
@@ -78,10 +93,21 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     // out of the registers the tile loop carries)
     __shared__ __attribute__((aligned(16))) int2 row_lohi[NW][16 * RBW];
 
+    const int wg = wg_id();
+    if constexpr (FEW > 0) {
+        typedef Few4Lds<D, FEW> F;
+        static_assert(KS == 1 && F::kBytes <= (int)sizeof(bufs), "few-row items use the tile buffers");
+        __shared__ typename F::Stats stats;
+        if (wg >= a.n_wgs) {
+            if (wg - a.n_wgs < args.few.n_items) few4_item<D, FEW>(args.few, wg - a.n_wgs, &bufs[0][0][0][0], stats);
+            return;
+        }
+    }
+
     // The planner's launch order names the (item, query head) of every
     // workgroup; it keeps the workgroups that read the same K/V pages on one
     // XCD.  Padding entries (item < 0) exit.
-    const int item = a.order[2 * wg_id()], head = a.order[2 * wg_id() + 1];
+    const int item = a.order[2 * wg], head = a.order[2 * wg + 1];
     if (item < 0) return;
     const int kvh = head / a.group;
     const WorkItem it = a.items[item];
