@@ -1,0 +1,96 @@
+"""Attention over a 4-bit cache on the plans that decide how it is launched: key
+groups, few-row items behind the tiles or the cascade, beside them on the side
+stream, or on their own, and references that keep moving."""
+import pytest
+
+import workloads as W
+from paper_2606_12688_amd import attn
+from tests.helpers import plan_for
+from tests.kv4_helpers import compare4, queries, random_pools, reference, run_kv4
+from tests.test_gpu_key_groups import _batch
+
+pytestmark = pytest.mark.gpu
+C, F = W.SEG_CAUSAL, W.SEG_FULL
+
+
+def _check(b, flags, label, seed=3, cascade=False):
+    k4, v4 = random_pools(b, seed)
+    q = queries(b, seed)
+    ref = reference(b, q, k4, v4)
+    for flag in flags:
+        compare4(b, *run_kv4(b, q, k4, v4, flag, cascade), ref, f"{label} flags {flag}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (7, 1), (6, 2)])
+def test_key_groups(hq, hkv, d):
+    _check(_batch(hq, hkv, d), (0, attn.FLAG_NO_SPLIT), f"key groups {hq}/{hkv} d{d}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_key_groups_beside_few_row_items(d):
+    kv = [900, 300, 77]
+    b = W.custom("groups_few", 4, 2, d, [900, 1, 1], kv, [[(0, n, C, 0)] for n in kv], [0] * 3, seed=d)
+    _check(b, (0, attn.FLAG_SERIAL), f"key groups beside few rows d{d}")
+
+
+def _mixed(hq, hkv, d, q, kv):
+    return W.custom("mixed_plan", hq, hkv, d, q, kv, [[(0, n, C, 0)] for n in kv], [0] * len(q), seed=d + hq)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,rows", [(8, 2, 1), (4, 4, 1), (8, 2, 6), (4, 4, 20), (16, 2, 7), (28, 4, 1)])
+def test_few_row_items_behind_the_tiles(hq, hkv, rows, d):
+    """Units of up to 16, 32 and 64 rows (the last go on their own stream at D = 64)."""
+    q = [1, 200, rows, 333, rows, 0, 150]
+    kv = [500, 200, 90, 600, 1000, 30, 150]
+    b = _mixed(hq, hkv, d, q, kv)
+    pl = plan_for(b, attn.FLAG_HOST_ONLY)
+    assert pl.stats()["decode_items"] > 0 and pl.stats()["prefill_items"] > 0
+    pl.destroy()
+    _check(b, (0, attn.FLAG_SERIAL, attn.FLAG_FORCE_SPLIT, attn.FLAG_NO_SPLIT), f"mixed {hq}/{hkv} {rows} rows d{d}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_tiles_than_the_gpu_holds(d):
+    q = [1] * 9 + [900] * 12
+    kv = [1000 + 37 * i for i in range(9)] + [900] * 12
+    _check(_mixed(16, 8, d, q, kv), (0,), f"many tiles d{d}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_cascade_with_tiles_and_few_row_items(d):
+    """Members of a prefix group, a prompt and decode steps in one plan."""
+    b = W.reduced("shared_prefix_decode_bf16")
+    for flags in (0, attn.FLAG_FORCE_SPLIT, attn.FLAG_CASCADE_ALL, attn.FLAG_SERIAL):
+        _check(b, (flags,), "cascade", cascade=True)
+    q, kv = [1, 1, 3, 150, 1], [400, 333, 350, 400, 700]
+    b = _mixed(8, 2, d, q, kv)
+    b.block_table[1, :20] = b.block_table[2, :20] = b.block_table[0, :20]
+    b.prefix_groups = [([0, 1, 2], 320)]
+    for flags in (0, attn.FLAG_FORCE_SPLIT, attn.FLAG_NO_SPLIT, attn.FLAG_SERIAL):
+        _check(b, (flags,), f"cascade and tiles d{d}", cascade=True)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("up", [1, -1])
+def test_growing_and_falling_scores(d, up):
+    """Key scales that double (or halve) every ten pages: references that move all
+    along, tiles redone exactly, pieces and key groups that end far apart."""
+    kv = [700, 900, 640, 333]
+    b = W.custom("growing", 4, 2, d, [700, 1, 90, 8], kv, [[(0, n, C, 0)] for n in kv], [0] * 4, seed=d)
+    k4, v4 = random_pools(b, 1)
+    for r in range(b.num_seqs):
+        for p in range((kv[r] + 15) // 16):
+            live = min(16, kv[r] - 16 * p)
+            scales = k4[b.block_table[r, p], :, 8 * d:].reshape(b.num_kv_heads, d // 32, 16)
+            scales[:, :, :live] += p // 10 if up > 0 else 6 - p // 10
+            k4[b.block_table[r, p], :, 8 * d:] = scales.reshape(b.num_kv_heads, -1)
+    q = queries(b, 2, scale=2.0 ** -6)  # the largest keys make scores as large as the bars assume
+    ref = reference(b, q, k4, v4)
+    for flag in (0, attn.FLAG_FORCE_SPLIT, attn.FLAG_NO_SPLIT):
+        compare4(b, *run_kv4(b, q, k4, v4, flag), ref, f"scores d{d} up {up} flags {flag}")
+    q = queries(b, 2, scale=4.0)  # and far apart
+    out, lse = run_kv4(b, q, k4, v4)
+    ro, rl, _ = reference(b, q, k4, v4)
+    assert abs(lse.cpu().numpy() - rl).max() <= 2.0 ** -3  # scores 256 times as large: 2^-11 * 2^8
