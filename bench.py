@@ -47,13 +47,16 @@ BOUND = {"tiny_causal_f32": "alu", "decode_bf16": "hbm", "text_latent_bf16": "mf
 KERNEL_NAMES = ["tile_kernel", "few_kernel", "f32_kernel", "merge_kernel", "cascade_kernel"]
 DOMINANT = {"tiny_causal_f32": 2, "decode_bf16": 1, "text_latent_bf16": 0, "stream_window_bf16": 1,
             "rollout_bf16": 0, "cfg_labels_bf16": 0, "shared_prefix_decode_bf16": 1, "serving_mix_bf16": 0}
-KERNEL_SRC = os.path.join(ROOT, "paper_2606_12688_amd", "csrc", "kernels.hip")
+KERNEL_SRC = [os.path.join(ROOT, "paper_2606_12688_amd", "csrc", f) for f in ("kernels.hip", "tile.h", "device.h")]
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "traffic.json")
 
 
 def kernel_source_sha() -> str:
-    with open(KERNEL_SRC, "rb") as f:
-        return hashlib.sha256(f.read()).hexdigest()[:16]
+    sha = hashlib.sha256()
+    for src in KERNEL_SRC:
+        with open(src, "rb") as f:
+            sha.update(f.read())
+    return sha.hexdigest()[:16]
 
 
 def kv_bytes(b, key_ranges) -> int:

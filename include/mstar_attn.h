@@ -32,6 +32,9 @@
  *   k_pages/v_pages [num_pages][page_size][Hkv][head_dim]   ("NHD")
  *   block_table   int32 [num_seqs][max_blocks_per_seq]
  *
+ * mstar_cache.h adds operators on such caches: one held in 4 bits, and block
+ * tables built on the GPU.
+ *
  * Error convention.  Every int-returning call returns MSTAR_OK (0) or a
  * negative MSTAR_ERR_* code and never throws or aborts; mstar_last_error()
  * then gives a message for the calling thread.

@@ -18,11 +18,15 @@ namespace {
 //    permute exchanges the halves.
 // A lane's share of out is then the D / 4 consecutive dims from G D / 4 on.
 //
-// Bound: HBM.  A step's registers take the next step's loads as soon as they are
-// read; larger steps (64 keys) or two and three steps in flight change nothing
-// (decode batch of 64: 42-46 us; 256 16-token chunks 82-99), but loads that the
-// compiler cannot count do (92 us for the chunks' 82).  Non-temporal loads of
-// the codes: 51 -> 46 us for 128 decode steps behind a shared prefix.
+// Bound: HBM.  Decode steps of 64 requests (28/4 heads, D = 128, 167 MB of cache)
+// take 36 us, 4.6 TB/s, of which some 5 us are a workgroup's start; reading their
+// pages without computing takes 33.  256 16-token chunks (290 MB) take 76 us, 3.8
+// TB/s; reading alone 69, computing alone 55.  A step's registers take the next step's loads as
+// soon as they are read; larger steps (64 keys) or two and three steps in flight
+// change nothing (decode 42-46 us with its merge, chunks 82-99), but loads in a
+// branch, which the compiler cannot count and waits for together, cost the
+// chunks 92 us for 82.  Non-temporal loads of the codes: 51 -> 46 us for 128
+// decode steps behind a shared prefix.
 // ---------------------------------------------------------------------------
 template <int D, int RB>
 struct Few4Lds {

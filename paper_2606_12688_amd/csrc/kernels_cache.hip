@@ -13,6 +13,11 @@ namespace {
 // 4 n + j holds dims [n D / 16, +D / 16) of a group's key j, so that its V words
 // are consecutive and its K words run over 64 (D = 128) or 32 bytes of each
 // piece.  The 32 dims of a scale are 4 (D = 128) or 8 neighbouring n.
+//
+// Bound: HBM and the chain of reads before it (item, request, rows and page
+// indices).  34816 rows of 4 heads at D = 128 (71 MB read, 19 MB written) take 24
+// us, 3.7 TB/s; with element-wise loads behind the page indices, and each code found
+// by comparisons, it was 40.
 // ---------------------------------------------------------------------------
 // A lane's D / 16 bf16 values as packed pairs.
 template <int D>
@@ -143,7 +148,7 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
 //
 // Bound: HBM, mostly the pages written.  Rows that the append reads and pages that
 // this writes are non-temporal: 34816 rows of 4 heads stored and read back (D =
-// 128, 180 MB) 48 -> 39 us.
+// 128, 180 MB) 48 -> 39 us, of which this kernel takes 15.4 (5.8 TB/s).
 // ---------------------------------------------------------------------------
 template <int D>
 __device__ __forceinline__ void store_word(bf16_t* out, uint32_t w, float s) {
@@ -188,8 +193,10 @@ __global__ __launch_bounds__(256) void unpack4_kernel(Unpack4Args a) {
 
 // ---------------------------------------------------------------------------
 // Block tables: a thread per new row.  The row that starts a page enters it; rows
-// of one page read the same entry of the free list, so no thread waits for
-// another.
+// of one page read the same entry of the free list, whose offset per request is in
+// the plan, so no thread waits for another.
+//
+// Bound: the launch (4.1 us for 64 rows, 4.7 for 307200 and 2.5 MB of slots).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void tables_kernel(TablesArgs a) {
     const int item = wg_id() * 16 + (thread_id() >> 4), r = thread_id() & 15;

@@ -9,4 +9,5 @@ hipError_t launch_tables(const TablesArgs&, hipStream_t) { return hipErrorNotSup
 hipError_t launch_tiles4(const KArgs&, int, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_cascade4(const KArgs&, int, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_few4(const KArgs&, int, int, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_mixed4(const KArgs&, const KArgs&, bool, int, int, hipStream_t) { return hipErrorNotSupported; }
 }  // namespace mstar
