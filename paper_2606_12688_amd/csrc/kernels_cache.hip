@@ -231,26 +231,38 @@ hipError_t launch_unpack4(const Unpack4Args& a, int head_dim, hipStream_t s) {
 }
 
 namespace {
-template <int MODE, int KS64, int KS128>
+// Keys per tile at D = 128: 32, with three workgroups per CU, or 64 with two
+// (half the barriers per key and twice the independent work per wave) where a
+// launch leaves a CU no more than two anyway: one prompt of 1500 tokens, 28/4 heads,
+// 45.3 -> 42.6 us; two of 1000 35.8 -> 33.3; one of 600 21.4 -> 20.5 (but 20 of 200,
+// 640 workgroups: 21.1 -> 26.8).  With key groups two of 64 keys for three of 32:
+// one prompt of 1000 tokens, 8/2 heads, 25.2 -> 24.4, 1500, 4/4, 29.3 -> 27.8; two of
+// 1846, 8/2, 38.7 -> 39.0.
+constexpr int kTwoPerCu = 512;
+
+template <int MODE, int BN128, int KS64, int KS128>
 hipError_t launch_tile4_mode(const KArgs& a, int head_dim, hipStream_t s) {
     const dim3 g((unsigned)a.n_wgs);
     return head_dim == 64 ? launch(tile_kernel<64, 2, kPool4, MODE, 64, KS64>, g, dim3(256 * KS64), a, s)
-                          : launch(tile_kernel<128, 2, kPool4, MODE, 32, KS128>, g, dim3(256 * KS128), a, s);
+                          : launch(tile_kernel<128, 2, kPool4, MODE, BN128, KS128>, g, dim3(256 * KS128), a, s);
+}
+template <int MODE>
+hipError_t launch_tile4_rows(const KArgs& a, int head_dim, hipStream_t s) {
+    if (a.key_groups) return launch_tile4_mode<MODE, 64, 4, 2>(a, head_dim, s);
+    return a.n_wgs <= kTwoPerCu ? launch_tile4_mode<MODE, 64, 1, 1>(a, head_dim, s)
+                                : launch_tile4_mode<MODE, 32, 1, 1>(a, head_dim, s);
 }
 }  // namespace
 
 // As launch_tiles, launch_cascade and launch_few for a 16-bit cache.
 hipError_t launch_tiles4(const KArgs& a, int head_dim, hipStream_t s) {
     if (a.n_items == 0) return hipSuccess;
-    const bool packed = a.group_inv != 0;
-    if (a.key_groups)
-        return packed ? launch_tile4_mode<kPacked, 4, 3>(a, head_dim, s) : launch_tile4_mode<kRows, 4, 3>(a, head_dim, s);
-    return packed ? launch_tile4_mode<kPacked, 1, 1>(a, head_dim, s) : launch_tile4_mode<kRows, 1, 1>(a, head_dim, s);
+    return a.group_inv != 0 ? launch_tile4_rows<kPacked>(a, head_dim, s) : launch_tile4_rows<kRows>(a, head_dim, s);
 }
 
 hipError_t launch_cascade4(const KArgs& a, int head_dim, hipStream_t s) {
     if (a.n_items == 0) return hipSuccess;
-    return launch_tile4_mode<kCascade, 1, 1>(a, head_dim, s);
+    return launch_tile4_mode<kCascade, 32, 1, 1>(a, head_dim, s);
 }
 
 namespace {

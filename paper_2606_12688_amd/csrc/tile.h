@@ -49,8 +49,8 @@ enum { kRows, kPacked, kCascade };
 
 // What it reads: a 16-bit pool of up to 2 GB or of any size, or a 4-bit pool.
 //
-// A 4-bit tile cannot go straight into LDS: a wave loads its share (D = 128: the
-// 16 keys of one page, K or V; D = 64: both) into registers a tile ahead, a lane
+// A 4-bit tile cannot go straight into LDS: a wave loads its share (of two pages the
+// 16 keys of one, K or V; of four, both of one) into registers a tile ahead, a lane
 // its D / 8 bytes of each record, and converts them into the same LDS image that
 // the direct loads of a 16-bit tile leave, so that each value is converted once
 // per workgroup and everything after it is the same.  Bound as the 16-bit instances
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
     constexpr int TB = BN * RBY;     // bytes of one K or V tile
     constexpr int PPT = BN / 16;     // pages per tile
     constexpr bool SMALL = CACHE == kPoolSmall;
-    static_assert(CACHE != kPool4 || (PPT == NW / 2 && D == 128) || (PPT == NW && D == 64), "shares of a 4-bit tile");
+    static_assert(CACHE != kPool4 || (PPT == NW / 2 && D == 128) || PPT == NW, "shares of a 4-bit tile");
     // two tile buffers per key group ([K, V] of its even and odd tiles): tile
     // t + 1 loads into one while tile t is read from the other
     __shared__ __attribute__((aligned(1024))) char bufs[2][KS][2][TB];
@@ -386,15 +386,26 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
 
     // ---- 4-bit loads and conversion ------------------------------------------
     // wave w's share of a tile: page w % PPT of it, K for the first PPT waves and
-    // V for the others (D = 128), or both (D = 64)
+    // V for the others (two pages), or both (four)
     typedef Record<D> R;
     constexpr bool BOTH = PPT == NW;
     const int share_page = wave % PPT;
     const bool share_v = wave >= PPT;
+    constexpr int NC4 = D / 32;  // dwords of codes per lane and record
     struct Raw {
-        uint4 code;           // D = 64: K in x and y, V in z and w
-        uint32_t scale, vs;   // D = 64: of K (one byte) and of V
+        uint32_t code[BOTH ? 2 * NC4 : NC4];  // with both: K, then V
+        uint32_t scale, vs;                   // with both: of K (one byte) and of V
     } raw;
+    auto load_codes = [&](__amdgpu_buffer_rsrc_t r, uint32_t* x) {
+        if constexpr (D == 128) {
+            const uint4 c = load16_at(r, lane * 16);
+            x[0] = c.x; x[1] = c.y; x[2] = c.z; x[3] = c.w;
+        } else {
+            typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+            const u32x2 c = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, lane * 8, 0, 0));
+            x[0] = c[0]; x[1] = c[1];
+        }
+    };
     // The item's page indices pass through two registers of 64 (a lane each): a
     // scalar load in the tile loop would make every wait for LDS reads a wait for
     // all of them.  Pages past the last one are -1, and no load sits in a branch,
@@ -412,20 +423,18 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
         page_err |= !ok && rel + share_page < n_pages;
         const size_t ofs = ok ? ((size_t)page * a.hkv + kvh) * R::kBytes : 0;
         const uint32_t nrec = ok ? (uint32_t)R::kBytes : 0u;  // else reads zeros
-        // four scale bytes of V; of K the one byte (D = 64), or those of keys n & ~3 .. n | 3
+        // four scale bytes of V; of K the one byte (with both), or those of keys n & ~3 .. n | 3
         const uint32_t kscale = R::kScales + (grp * (D / 4) / 32) * 16 + (BOTH ? n : n & ~3);
         const uint32_t vscale = R::scale(4 * grp, n);
         if constexpr (BOTH) {
             const __amdgpu_buffer_rsrc_t rk = page_rsrc(kbase, ofs, nrec), rv = page_rsrc(vbase, ofs, nrec);
-            typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-            const u32x2 kc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rk, lane * 8, 0, 0));
-            const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rv, lane * 8, 0, 0));
-            raw.code = uint4{kc[0], kc[1], vc[0], vc[1]};
+            load_codes(rk, raw.code);
+            load_codes(rv, raw.code + NC4);
             raw.scale = __builtin_amdgcn_raw_buffer_load_b8(rk, (int)kscale, 0, 0);
             raw.vs = __builtin_amdgcn_raw_buffer_load_b32(rv, (int)vscale, 0, 0);
         } else {
             const __amdgpu_buffer_rsrc_t r = page_rsrc(share_v ? vbase : kbase, ofs, nrec);
-            raw.code = load16_at(r, lane * 16);
+            load_codes(r, raw.code);
             raw.scale = __builtin_amdgcn_raw_buffer_load_b32(r, (int)(share_v ? vscale : kscale), 0, 0);
         }
     };
@@ -444,16 +453,21 @@ __global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void ti
         char* to = &dst[0][0];
         if constexpr (BOTH) {
             const float sk = scale_of(raw.scale);
-            *reinterpret_cast<bf16x8*>(to + k_at) = eight_of(raw.code.x, sk);
-            *reinterpret_cast<bf16x8*>(to + (k_at ^ 0x10)) = eight_of(raw.code.y, sk);
+#pragma unroll
+            for (int i = 0; i < NC4; ++i)
+                *reinterpret_cast<bf16x8*>(to + (k_at ^ (i * 0x10))) = eight_of(raw.code[i], sk);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t w = (i >> 1) ? raw.code.w : raw.code.z;
                 const float sv = scale_of(v_scale(raw.vs, i));
-                *reinterpret_cast<bf16x4*>(to + (v_at ^ v_flip(i))) = (i & 1) ? four_of<2>(w, sv) : four_of<0>(w, sv);
+                if constexpr (D == 128) {
+                    *reinterpret_cast<bf16x8*>(to + (v_at ^ v_flip(i))) = eight_of(raw.code[NC4 + i], sv);
+                } else {
+                    const uint32_t w = raw.code[NC4 + (i >> 1)];
+                    *reinterpret_cast<bf16x4*>(to + (v_at ^ v_flip(i))) = (i & 1) ? four_of<2>(w, sv) : four_of<0>(w, sv);
+                }
             }
         } else {
-            const uint32_t w[4] = {raw.code.x, raw.code.y, raw.code.z, raw.code.w};
+            const uint32_t* w = raw.code;
             const uint32_t sc = __builtin_amdgcn_perm(raw.scale, raw.scale, pick4);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
