@@ -237,7 +237,9 @@ namespace {
 // 45.3 -> 42.6 us; two of 1000 35.8 -> 33.3; one of 600 21.4 -> 20.5 (but 20 of 200,
 // 640 workgroups: 21.1 -> 26.8).  With key groups two of 64 keys for three of 32:
 // one prompt of 1000 tokens, 8/2 heads, 25.2 -> 24.4, 1500, 4/4, 29.3 -> 27.8; two of
-// 1846, 8/2, 38.7 -> 39.0.
+// 1846, 8/2, 38.7 -> 39.0.  Three key groups at D = 64, where a fourth leaves the
+// conversion too few registers: one prompt of 700 tokens, 16/8 heads, 17.6 -> 14.8,
+// of 1500 28.0 -> 24.7.
 constexpr int kTwoPerCu = 512;
 
 template <int MODE, int BN128, int KS64, int KS128>
@@ -248,7 +250,7 @@ hipError_t launch_tile4_mode(const KArgs& a, int head_dim, hipStream_t s) {
 }
 template <int MODE>
 hipError_t launch_tile4_rows(const KArgs& a, int head_dim, hipStream_t s) {
-    if (a.key_groups) return launch_tile4_mode<MODE, 64, 4, 2>(a, head_dim, s);
+    if (a.key_groups) return launch_tile4_mode<MODE, 64, 3, 2>(a, head_dim, s);
     return a.n_wgs <= kTwoPerCu ? launch_tile4_mode<MODE, 64, 1, 1>(a, head_dim, s)
                                 : launch_tile4_mode<MODE, 32, 1, 1>(a, head_dim, s);
 }

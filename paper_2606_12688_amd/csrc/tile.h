@@ -72,7 +72,7 @@ __device__ __forceinline__ const KArgs& tile_args(const KArgs& a) { return a; }
 __device__ __forceinline__ const KArgs& tile_args(const MixedArgs& a) { return a.tile; }
 
 template <int D, int RBW, int CACHE, int MODE, int BN, int KS, int FEW = 0>
-__global__ __launch_bounds__(256 * KS, D == 64 ? 4 : (BN == 32 ? 3 : 2)) void tile_kernel(
+__global__ __launch_bounds__(256 * KS, CACHE == kPool4 && KS > 1 ? KS : D == 64 ? 4 : (BN == 32 ? 3 : 2)) void tile_kernel(
     std::conditional_t<FEW == 0, KArgs, MixedArgs> args) {
     const KArgs& a = tile_args(args);
     static_assert(BN == 32 || BN == 64, "tile sizes");
