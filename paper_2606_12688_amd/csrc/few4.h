@@ -28,9 +28,8 @@ namespace {
 // chunks 92 us for 82.  Non-temporal loads of the codes: 51 -> 46 us for 128
 // decode steps behind a shared prefix.
 // ---------------------------------------------------------------------------
-template <int D, int RB>
+template <int D, int RB, int NW>  // NW waves
 struct Few4Lds {
-    static constexpr int NW = 4;              // waves
     static constexpr int PC = D / 16;         // 16-byte pieces of a lane's results per row block
     static constexpr bool QLDS = RB * D >= 256;  // Q in LDS: in registers it would cost a wave per SIMD
     // a wave's results while they are combined; before that, Q
@@ -43,11 +42,11 @@ struct Few4Lds {
 };
 
 // Work item `item` of the launch; `lds` has Few4Lds::kBytes, 16-byte aligned.
-template <int D, int RB>
-__device__ __forceinline__ void few4_item(const KArgs& a, int item, char* lds, typename Few4Lds<D, RB>::Stats& stats) {
+template <int D, int RB, int NW>
+__device__ __forceinline__ void few4_item(const KArgs& a, int item, char* lds, typename Few4Lds<D, RB, NW>::Stats& stats) {
     typedef Record<D> R;
-    typedef Few4Lds<D, RB> L4;
-    constexpr int NW = L4::NW, PC = L4::PC;
+    typedef Few4Lds<D, RB, NW> L4;
+    constexpr int PC = L4::PC;
     constexpr bool QLDS = L4::QLDS;
     constexpr int PG = 2, SK = 16 * PG;  // pages and keys of a step
     constexpr int DS = D / 32, DB = D / 16;
@@ -306,11 +305,11 @@ __device__ __forceinline__ void few4_item(const KArgs& a, int item, char* lds, t
     }
 }
 
-template <int D, int RB>
-__global__ __launch_bounds__(256, RB == 1 ? 4 : (RB == 2 ? 3 : 2)) void few4_kernel(KArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[Few4Lds<D, RB>::kBytes];
-    __shared__ typename Few4Lds<D, RB>::Stats stats;
-    few4_item<D, RB>(a, wg_id(), lds, stats);
+template <int D, int RB, int NW>
+__global__ __launch_bounds__(64 * NW, RB == 1 ? 4 : (RB == 2 ? 3 : 2)) void few4_kernel(KArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[Few4Lds<D, RB, NW>::kBytes];
+    __shared__ typename Few4Lds<D, RB, NW>::Stats stats;
+    few4_item<D, RB, NW>(a, wg_id(), lds, stats);
 }
 
 }  // namespace

@@ -290,16 +290,31 @@ hipError_t launch_mixed4(const KArgs& tile, const KArgs& few, bool cascade, int 
     return rb == 1 ? launch_mixed4_rows<1>(a, cascade, head_dim, s) : launch_mixed4_rows<2>(a, cascade, head_dim, s);
 }
 
+namespace {
+// Eight waves per item, for four, where the items leave a CU room for them (as many
+// as its registers hold: two workgroups, or one of more rows): 64 decode steps over
+// 4000 keys, 16/8 heads at D = 64 (512 items), 37.8 -> 30.7 us; 128 over 1500, 28/4 at
+// D = 128 (512), 22.1 -> 20.9; 32 16-token chunks over 2000, 16/8 (256), 25.1 -> 20.1;
+// one over 1500 keys (24) 8.9 -> 8.7.  Past that they lose: 50 over 3000, 12/12 (600),
+// 47.9 -> 52.1.
+template <int D, int RB>
+hipError_t launch_few4_rows(const KArgs& a, hipStream_t s) {
+    constexpr int kPerCu = RB == 1 || (D == 64 && RB == 2) ? 2 : 1;
+    const dim3 g(a.n_items);
+    return a.n_items <= 256 * kPerCu ? launch(few4_kernel<D, RB, 8>, g, dim3(512), a, s)
+                                     : launch(few4_kernel<D, RB, 4>, g, dim3(256), a, s);
+}
+}  // namespace
+
 hipError_t launch_few4(const KArgs& a, int head_dim, int rb, hipStream_t s) {
     if (a.n_items == 0) return hipSuccess;
-    const dim3 g(a.n_items), b(256);
     if (head_dim == 64) {
-        if (rb == 1) return launch(few4_kernel<64, 1>, g, b, a, s);
-        else if (rb == 2) return launch(few4_kernel<64, 2>, g, b, a, s);
-        else return launch(few4_kernel<64, 4>, g, b, a, s);
+        if (rb == 1) return launch_few4_rows<64, 1>(a, s);
+        else if (rb == 2) return launch_few4_rows<64, 2>(a, s);
+        else return launch_few4_rows<64, 4>(a, s);
     } else {
-        if (rb == 1) return launch(few4_kernel<128, 1>, g, b, a, s);
-        else return launch(few4_kernel<128, 2>, g, b, a, s);
+        if (rb == 1) return launch_few4_rows<128, 1>(a, s);
+        else return launch_few4_rows<128, 2>(a, s);
     }
 }
 

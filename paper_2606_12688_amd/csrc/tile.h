@@ -99,11 +99,11 @@ __global__ __launch_bounds__(256 * KS, CACHE == kPool4 && KS > 1 ? KS : D == 64 
 
     const int wg = wg_id();
     if constexpr (FEW > 0) {
-        typedef Few4Lds<D, FEW> F;
+        typedef Few4Lds<D, FEW, NW> F;
         static_assert(KS == 1 && F::kBytes <= (int)sizeof(bufs), "few-row items use the tile buffers");
         __shared__ typename F::Stats stats;
         if (wg >= a.n_wgs) {
-            if (wg - a.n_wgs < args.few.n_items) few4_item<D, FEW>(args.few, wg - a.n_wgs, &bufs[0][0][0][0], stats);
+            if (wg - a.n_wgs < args.few.n_items) few4_item<D, FEW, NW>(args.few, wg - a.n_wgs, &bufs[0][0][0][0], stats);
             return;
         }
     }
