@@ -292,11 +292,16 @@ hipError_t launch_mixed4(const KArgs& tile, const KArgs& few, bool cascade, int 
 
 namespace {
 // Eight waves per item, for four, where the items leave a CU room for them (as many
-// as its registers hold: two workgroups, or one of more rows): 64 decode steps over
-// 4000 keys, 16/8 heads at D = 64 (512 items), 37.8 -> 30.7 us; 128 over 1500, 28/4 at
-// D = 128 (512), 22.1 -> 20.9; 32 16-token chunks over 2000, 16/8 (256), 25.1 -> 20.1;
-// one over 1500 keys (24) 8.9 -> 8.7.  Past that they lose: 50 over 3000, 12/12 (600),
-// 47.9 -> 52.1.
+// as its registers hold: two workgroups, or one of more rows).  us with four -> eight:
+//   D = 64, 16/8 heads: 64 decode steps over 4000 keys (512 items)   39.0 -> 31.3
+//                       64 12-token chunks over 2000 (512)           27.8 -> 24.3
+//   D = 128, 28/4:      128 decode steps over 1500 (512)             22.6 -> 20.8
+//                       one over 1500 (24)                            9.1 ->  8.8
+//                       8 over 2000 (256)                             9.6 ->  9.6
+//   D = 128, 16/8:      32 16-token chunks over 2000 (256)           25.7 -> 20.7
+// Past that they lose, at D = 64 and 12/12 heads:
+//                       50 decode steps over 3000 (600)              33.4 -> 35.1
+//                       64 over 600 (768)                            10.6 -> 13.6
 template <int D, int RB>
 hipError_t launch_few4_rows(const KArgs& a, hipStream_t s) {
     constexpr int kPerCu = RB == 1 || (D == 64 && RB == 2) ? 2 : 1;
