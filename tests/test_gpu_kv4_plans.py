@@ -94,3 +94,32 @@ def test_growing_and_falling_scores(d, up):
     out, lse = run_kv4(b, q, k4, v4)
     ro, rl, _ = reference(b, q, k4, v4)
     assert abs(lse.cpu().numpy() - rl).max() <= 2.0 ** -3  # scores 256 times as large: 2^-11 * 2^8
+
+
+# how many requests of how many query rows: units of up to 16, 32 and 64 rows (the last at D = 64 only)
+@pytest.mark.parametrize("few", [True, False], ids=["few_items", "many_items"])
+@pytest.mark.parametrize("d,hq,hkv,rows", [(64, 16, 8, 1), (128, 28, 4, 1), (64, 12, 12, 5), (128, 8, 8, 16),
+                                           (64, 16, 8, 12), (128, 28, 4, 4), (64, 28, 4, 8), (64, 8, 8, 50)])
+def test_few_row_items_on_their_own(d, hq, hkv, rows, few):
+    """Launches that leave a CU one workgroup at most, and more than it holds of two: both sizes of a workgroup."""
+    n = 2 if few else 520 // hkv + 1
+    kv = [rows + (37 * i) % 230 for i in range(n - 1)] + [1100]
+    b = W.custom("few_alone", hq, hkv, d, [rows] * n, kv, [[(0, x, C, 0)] for x in kv], [0] * n, seed=rows)
+    pl = plan_for(b, attn.FLAG_HOST_ONLY | attn.FLAG_NO_SPLIT)
+    s = pl.stats()
+    pl.destroy()
+    assert s["prefill_items"] == 0 and (0 < s["decode_items"] <= 256 if few else s["decode_items"] > 512), s
+    _check(b, (attn.FLAG_NO_SPLIT, 0), f"few alone {hq}/{hkv} {rows} rows d{d} x {n}")
+
+
+@pytest.mark.parametrize("few", [True, False], ids=["few_tiles", "many_tiles"])
+@pytest.mark.parametrize("d,hq,hkv", [(64, 8, 8), (128, 8, 8), (64, 28, 4), (128, 28, 4), (128, 12, 12)])
+def test_tiles_on_their_own(d, hq, hkv, few):
+    """Tiles without key groups that leave a CU two workgroups at most, and more."""
+    lens = [170, 333] if few else [170 + 17 * i for i in range(12)] * (1 if hq == 28 else 3)
+    b = W.custom("tiles_alone", hq, hkv, d, lens, lens, [[(0, x, C, 0)] for x in lens], [0] * len(lens), seed=d)
+    pl = plan_for(b, attn.FLAG_HOST_ONLY)
+    s, wgs = pl.stats(), len(pl.tile_order())
+    pl.destroy()
+    assert s["decode_items"] == 0 and (0 < wgs <= 512 if few else wgs > 512), (s, wgs)
+    _check(b, (0,), f"tiles alone {hq}/{hkv} d{d} x {len(lens)}")
