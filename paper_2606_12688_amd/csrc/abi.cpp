@@ -394,6 +394,7 @@ int mstar::run_fwd(const Launchers& kernels, const mstar_plan* plan, const void*
         a.n_wgs = (int32_t)(h.tile_order.size() / 2);
         a.key_groups = h.key_groups;
         a.span_step = std::max(512, h.tile_span / 4);
+        a.span = h.tile_span;
         a.done = done(0);
         MSTAR_MARK(events_before, 0);
         e = with_tiles ? kernels.mixed(a, few, false, D, h.decode_rb, s) : kernels.tiles(a, D, s);
@@ -407,6 +408,7 @@ int mstar::run_fwd(const Launchers& kernels, const mstar_plan* plan, const void*
         a.n_wgs = (int32_t)(h.casc_order.size() / 2);
         a.key_groups = 0;
         a.span_step = std::max(512, h.casc_span / 4);
+        a.span = h.casc_span;
         a.rows = reinterpret_cast<const int32_t*>(blob + plan->off_casc_rows);
         a.done = done(4);
         MSTAR_MARK(events_before, 4);

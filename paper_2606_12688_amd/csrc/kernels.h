@@ -32,6 +32,7 @@ struct KArgs {
     float sm_scale;
     float scale_log2;  // sm_scale * log2(e)
     hipEvent_t done;  // host side: NULL, or an event that completes with the kernel (not under capture)
+    int32_t span;     // host side: keys of the longest multi-row item
 };
 
 // A launch that holds both multi-row work and few-row items (4-bit cache only).

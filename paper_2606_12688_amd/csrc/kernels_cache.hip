@@ -268,11 +268,29 @@ hipError_t launch_cascade4(const KArgs& a, int head_dim, hipStream_t s) {
 }
 
 namespace {
+// At D = 128 few-row items take the tiles' LDS, so tiles of 64 keys also halve how many
+// items a CU holds.  They are taken where few workgroups wait for that (three a CU,
+// tiles and items together), us with 32 -> 64 keys: 4 decode steps beside three
+// prompts of 400 tokens, 16/8 heads (192 tiles, 544 items), 24.9 -> 23.1; beside two of
+// 600, 28/4 (280, 272), 30.2 -> 29.0; 40 behind a prefix of 16384, 28/4 (264, 296),
+// 39.0 -> 36.3.  From there to 900 either wins (4 beside one of 1500, 16/8, 256 and 544,
+// 45.5 -> 40.9; 32 beside two of 300, 28/4, 168 and 708, 23.5 -> 26.2), past it 32 keys
+// (32 beside three of 400, 28/4, 392 and 708, 30.4 -> 32.9).  Or where a cascade's
+// longest item, a chain of its keys, outlasts the items' turns: its keys are at least
+// as many as there are items.  128 behind 24576, 28/4 (2389 keys, 932 items), 101.6 ->
+// 94.8; 200 behind 16384, 16/8 (2048, 1600), 72.1 -> 65.0; but 200 behind 8192 (1024,
+// 1600) 46.1 -> 50.5 and 128 behind 4096, 28/4 (394, 932), 34.3 -> 35.1.
+constexpr int kThreePerCu = 768;
+
 template <int MODE, int RB>
 hipError_t launch_mixed4_mode(const MixedArgs& a, int head_dim, hipStream_t s) {
     const dim3 g((unsigned)a.tile.n_wgs + (unsigned)a.few.n_items), b(256);
-    return head_dim == 64 ? launch(tile_kernel<64, 2, kPool4, MODE, 64, 1, RB>, g, b, a, s)
-                          : launch(tile_kernel<128, 2, kPool4, MODE, 32, 1, RB>, g, b, a, s);
+    if (head_dim == 64) return launch(tile_kernel<64, 2, kPool4, MODE, 64, 1, RB>, g, b, a, s);
+    const bool long_keys = a.tile.n_wgs <= kTwoPerCu &&
+                           ((int64_t)a.tile.n_wgs + a.few.n_items <= kThreePerCu ||
+                            (MODE == kCascade && a.tile.span >= a.few.n_items));
+    return long_keys ? launch(tile_kernel<128, 2, kPool4, MODE, 64, 1, RB>, g, b, a, s)
+                     : launch(tile_kernel<128, 2, kPool4, MODE, 32, 1, RB>, g, b, a, s);
 }
 template <int RB>
 hipError_t launch_mixed4_rows(const MixedArgs& a, bool cascade, int head_dim, hipStream_t s) {

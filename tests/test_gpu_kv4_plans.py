@@ -123,3 +123,40 @@ def test_tiles_on_their_own(d, hq, hkv, few):
     pl.destroy()
     assert s["decode_items"] == 0 and (0 < wgs <= 512 if few else wgs > 512), (s, wgs)
     _check(b, (0,), f"tiles alone {hq}/{hkv} d{d} x {len(lens)}")
+
+
+@pytest.mark.parametrize("few", [True, False], ids=["few_items", "many_items"])
+@pytest.mark.parametrize("cascade", [False, True], ids=["tiles", "cascade"])
+@pytest.mark.parametrize("d,hq,hkv,rows", [(128, 8, 2, 1), (128, 8, 8, 1), (128, 8, 2, 6), (128, 8, 8, 20), (64, 8, 4, 1)])
+def test_mixed_launches_of_few_and_of_many_items(d, hq, hkv, rows, cascade, few):
+    """Few-row items behind tiles, or behind a cascade (of one prefix for all of
+    them), on both sides of three workgroups a CU."""
+    n = 5 if few else 780 // hkv + 1
+    kv = [352 + rows + (29 * i) % 120 for i in range(n)]
+    q = [rows] * n
+    if not cascade:
+        q, kv = q + [200, 333], kv + [450, 333]
+    b = _mixed(hq, hkv, d, q, kv)
+    if cascade:
+        b.block_table[:, :20] = b.block_table[0, :20]
+        b.prefix_groups = [(list(range(n)), 320)]
+    pl = plan_for(b, attn.FLAG_HOST_ONLY | attn.FLAG_NO_SPLIT, cascade=cascade)
+    s, wgs = pl.stats(), len(pl.tile_order(cascade))
+    pl.destroy()
+    assert s["decode_items"] > 0 and 0 < wgs <= 512, (s, wgs)
+    assert (wgs + s["decode_items"] <= 768) == few, (s, wgs)
+    _check(b, (attn.FLAG_NO_SPLIT, 0), f"mixed {hq}/{hkv} {rows} rows d{d} x {n} cascade {cascade}", cascade=cascade)
+
+
+def test_a_cascade_of_more_keys_than_items():
+    """A launch of many items whose cascade item is longer still."""
+    n, prefix = 800, 1600
+    kv = [prefix + 1 + (7 * i) % 40 for i in range(n)]
+    b = _mixed(2, 1, 128, [1] * n, kv)
+    b.block_table[:, :prefix // 16] = b.block_table[0, :prefix // 16]
+    b.prefix_groups = [(list(range(n)), prefix)]
+    pl = plan_for(b, attn.FLAG_HOST_ONLY | attn.FLAG_NO_SPLIT, cascade=True)
+    s, wgs = pl.stats(), len(pl.tile_order(True))
+    pl.destroy()
+    assert s["decode_items"] == n and 0 < wgs <= 512, (s, wgs)
+    _check(b, (attn.FLAG_NO_SPLIT, 0), f"cascade of {prefix} keys, {n} items", cascade=True)
