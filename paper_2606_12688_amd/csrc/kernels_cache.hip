@@ -233,9 +233,10 @@ hipError_t launch_unpack4(const Unpack4Args& a, int head_dim, hipStream_t s) {
 namespace {
 // Keys per tile at D = 128: 32, with three workgroups per CU, or 64 with two
 // (half the barriers per key and twice the independent work per wave) where a
-// launch leaves a CU no more than two anyway: one prompt of 1500 tokens, 28/4 heads,
-// 45.3 -> 42.6 us; two of 1000 35.8 -> 33.3; one of 600 21.4 -> 20.5 (but 20 of 200,
-// 640 workgroups: 21.1 -> 26.8).  With key groups two of 64 keys for three of 32:
+// launch leaves a CU no more than two anyway: two prompts of 1000 tokens, 28/4 heads
+// (448 workgroups), 35.8 -> 33.3 us; one of 600 (168) 21.4 -> 20.5.  Past that either
+// wins, the losses being larger: one of 1500, 28/4 (560), 45.3 -> 42.6, eight of 300
+// (672) 24.4 -> 23.4, but 20 of 200, 16/8 (640), 21.1 -> 26.8.  With key groups two of 64 keys for three of 32:
 // one prompt of 1000 tokens, 8/2 heads, 25.2 -> 24.4, 1500, 4/4, 29.3 -> 27.8; two of
 // 1846, 8/2, 38.7 -> 39.0.  Three key groups at D = 64, where a fourth leaves the
 // conversion too few registers: one prompt of 700 tokens, 16/8 heads, 17.6 -> 14.8,
