@@ -28,7 +28,8 @@
  * magnitude, NaN is stored as 0, and an infinity or NaN also sets
  * MSTAR_DEVERR_NONFINITE in the plan's error word: attended pages hold finite
  * values only, whatever keys a row may not see.  Scale bytes above 252 (never
- * stored) read as unspecified values.
+ * stored) read as unspecified values.  Attention takes less than can be stored:
+ * see mstar_kv4_fwd.
  */
 #ifndef MSTAR_CACHE_H
 #define MSTAR_CACHE_H
@@ -59,9 +60,14 @@ int mstar_kv4_append(const mstar_plan_t* plan, const void* k_new, const void* v_
  * included), masks, q, out, lse, workspace, streams and capture, with k_pages /
  * v_pages 4-bit pools.  out and lse are the attention over the values that the
  * cache stands for; scores, softmax statistics and sums are fp32, the
- * probabilities enter the value product in bf16.  Errors as mstar_attn_fwd,
- * plus UNSUPPORTED (a plan of the fp32 dtype) and INVALID_ARG (the plan's device
- * is not the current one). */
+ * probabilities enter the value product in bf16.  That holds for rows whose
+ * scores q . k are finite in fp32 and which see values of V up to 2^64 in
+ * magnitude, at any length.  Weights are sums of powers relative to an earlier
+ * maximum, divided out at the end: with larger values they may overflow, and out
+ * of a row that sees one is unspecified (so is that of a row that sees a stored
+ * infinity, of largest magnitude).  Rows that do not see it are not touched by
+ * it.  Errors as mstar_attn_fwd, plus UNSUPPORTED (a plan of the fp32 dtype) and
+ * INVALID_ARG (the plan's device is not the current one). */
 int mstar_kv4_fwd(const mstar_plan_t* plan, const void* q, const void* k_pages, const void* v_pages,
                   const int32_t* block_table, void* out, float* lse, void* workspace, size_t workspace_bytes,
                   hipStream_t stream);

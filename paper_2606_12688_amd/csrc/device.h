@@ -239,7 +239,11 @@ __device__ __forceinline__ void softmax_fixed(f32x4 (&s)[RB][NB], float c, const
 }
 // Bound on a lane's partial sum of one tile under the fixed reference: below
 // it every probability is below 2^32, far from overflow of the sums and the
-// weighted values; at or above it (or inf / NaN) the tile is redone exactly.
+// weighted values; at or above it (or inf / NaN) the tile is redone exactly.  A
+// row's weights then sum to less than 2^60 over any 2^31 keys (2^26 tiles of 32, four
+// lanes each), so that weighted sums of values up to 2^64 stay below 2^124: the
+// range that a 4-bit cache states, whose format reaches 6 * 2^125 (values of
+// 2^100 under scores that grow by a few units gave infinities).
 constexpr float kFixedTileLimit = 4294967296.0f;  // 2^32
 
 template <int D>

@@ -1,6 +1,6 @@
 """Outputs (not only lse) of attention over a 4-bit cache whose scores are large,
 far apart and moving, so that references move by large steps and tiles are redone
-exactly.
+exactly, and under the largest values that attention takes.
 
 Bars.  With u = 2^-24, a score is a sum of d fp32 products (each exact: 8 by 2
 significant bits) taken in fp32, so off by at most 2 d u A, where A is the sum of
@@ -19,6 +19,7 @@ import pytest
 
 import workloads as W
 from oracle import kv4_read, kv4_values
+from oracle.kv4 import nibble_at, scale_at
 from paper_2606_12688_amd import attn
 from tests.helpers import host64
 from tests.kv4_helpers import queries, random_pools, run_kv4
@@ -113,3 +114,32 @@ def test_growing_scores_in_mixed_launches_and_cascades(d):
     k4, v4 = random_pools(b, 1)
     _ramp(b, k4, True, 8)
     _check(b, queries(b, 2, scale=4.0), k4, v4, f"mixed d{d}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_up_to_2_64(d):
+    """Values of up to 6 * 2^61 under scores that grow past a row's reference."""
+    b = _batch(d)
+    k4, v4 = random_pools(b, 1)
+    _ramp(b, k4, True, 20)
+    _, v4 = random_pools(b, 2, exponents=(61, 62))
+    for scale in (0.25, 1.0, 4.0):
+        _check(b, queries(b, 2, scale=scale), k4, v4, f"values of 2^61 d{d} scale {scale}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_do_not_see_the_largest_values(d):
+    """A key whose values are of the largest magnitude (a stored infinity): rows before it are as without it."""
+    b = _batch(d, kv=(333, 150), q=(333, 20), hq=8)
+    k4, v4 = random_pools(b, 1)
+    far = {0: 200, 1: 140}  # of each request, the key
+    rows = np.concatenate([np.arange(far[0]), 333 + np.arange(far[1] - 130)])
+    ro, bar, rl, lbar = (x[rows] for x in _causal(b, queries(b, 2), k4, v4))
+    for r, key in far.items():
+        page, slot = b.block_table[r, key // 16], key % 16
+        v4[page][:, scale_at(d)[slot]] = 252
+        v4[page][:, np.unique(nibble_at("v", d)[slot] // 2)] = 0x7F
+    for flag in FLAGS:
+        out, lse = run_kv4(b, queries(b, 2), k4, v4, flag)
+        o, l = host64(out)[rows], host64(lse)[rows]
+        assert (np.abs(o - ro) <= bar).all() and (np.abs(l - rl) <= lbar).all(), f"d{d} flags {flag}"
