@@ -274,7 +274,8 @@ int mstar_attn_fwd_noalloc(const mstar_plan_t* plan, const void* q, const void* 
 
 /* Synchronize `stream`, then read and clear the plan's sticky device error
  * word into *error_bits (MSTAR_DEVERR_* bits; 0 = no error seen).  Returns
- * INVALID_ARG if a bit was set, OK otherwise, HIP on a runtime failure. */
+ * INVALID_ARG if a bit was set (the message names every one), OK otherwise, HIP on a
+ * runtime failure. */
 int mstar_attn_check(mstar_plan_t* plan, hipStream_t stream, int32_t* error_bits);
 
 /* Planner statistics (host side; no device access). */

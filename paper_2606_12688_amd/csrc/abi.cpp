@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "mstar_attn.h"
+#include "mstar_cache.h"
 #include "plan.h"
 
 using mstar::PlanBlock;
@@ -543,9 +544,11 @@ MSTAR_EXPORT int mstar_attn_check(mstar_plan_t* plan, hipStream_t stream, int32_
         const int32_t zero = 0;
         e = hipMemcpy(d_err, &zero, sizeof zero, hipMemcpyHostToDevice);
         if (e != hipSuccess) return hip_fail(e, "error word clear");
-        return fail(MSTAR_ERR_INVALID_ARG, (v & MSTAR_DEVERR_PAGE_RANGE)
-                                               ? "a block-table entry was outside [0, num_pages)"
-                                               : "a new key or value was infinite or not a number");
+        std::string msg;
+        if (v & MSTAR_DEVERR_PAGE_RANGE) msg = "a block-table entry was outside [0, num_pages)";
+        if (v & MSTAR_DEVERR_NONFINITE)
+            msg += std::string(msg.empty() ? "" : "; ") + "a new key or value was infinite or not a number";
+        return fail(MSTAR_ERR_INVALID_ARG, msg);
     }
     return MSTAR_OK;
 }
