@@ -276,11 +276,19 @@ namespace {
 // 600, 28/4 (280, 272), 30.2 -> 29.0; 40 behind a prefix of 16384, 28/4 (264, 296),
 // 39.0 -> 36.3.  From there to 900 either wins (4 beside one of 1500, 16/8, 256 and 544,
 // 45.5 -> 40.9; 32 beside two of 300, 28/4, 168 and 708, 23.5 -> 26.2), past it 32 keys
-// (32 beside three of 400, 28/4, 392 and 708, 30.4 -> 32.9).  Or where a cascade's
-// longest item, a chain of its keys, outlasts the items' turns: its keys are at least
-// as many as there are items.  128 behind 24576, 28/4 (2389 keys, 932 items), 101.6 ->
-// 94.8; 200 behind 16384, 16/8 (2048, 1600), 72.1 -> 65.0; but 200 behind 8192 (1024,
-// 1600) 46.1 -> 50.5 and 128 behind 4096, 28/4 (394, 932), 34.3 -> 35.1.
+// (32 beside three of 400, 28/4, 392 and 708, 30.4 -> 32.9).
+// Or where a cascade's longest item has at least as many keys as there are few-row
+// items.  The item is a chain of its keys, which longer tiles shorten; the items' turns
+// grow with their number and with the keys of each, which the rule does not see, so
+// the ratio is a fit that errs to 32 keys.  Above it 64 won in each of seven cascades
+// (128 behind 12288, 28/4, 1280 keys and 908 items, 61.9 -> 57.1; 200 behind 16384,
+// 16/8, 2048 and 1600, 69.0 -> 61.9; 100 behind 32768, 8/8, 1024 and 800, 44.6 -> 41.8;
+// 600 behind 4096, 8/1, 640 and 600, 37.8 -> 37.2).  Below it either wins: gains not
+// taken are 128 behind 6144 and 8192, 28/4 (640 and 832, 908), 41.5 -> 39.0 and 47.8 ->
+// 44.7, and 300 behind 3584 (896, 1200), 52.5 -> 47.7; losses spared 200 behind 8192,
+// 16/8 (1024, 1600), 45.2 -> 50.4, behind 4096 (512, 1600) 38.4 -> 43.9, 100 behind
+// 16384, 8/8 (512, 800), 33.1 -> 36.3, and 300 behind 2048, 28/4 (512, 1200), 40.2 ->
+// 42.1.
 constexpr int kThreePerCu = 768;
 
 template <int MODE, int RB>
