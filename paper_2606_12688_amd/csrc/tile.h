@@ -42,6 +42,14 @@ constexpr int kTileKeysD128 = MSTAR_TILE_KEYS_D128;
 // tile buffers of their own, and their results are added up in LDS at the end.
 // For launches that leave a CU at most one workgroup: it then has as many waves
 // as KS workgroups would give it, on a KS-th of the keys.
+// 4-bit tiles at d = 64 hold more addresses than 128 VGPRs take: 2-4 registers spill
+// (mixed launches, FEW below: 4 in a cascade, 9 packed, 12 by rows; by rows at d =
+// 128 with 32 keys 4), and a reload in the loop waits for the tile ahead's loads too.
+// At three waves per SIMD nothing spills, and either wins, us with four -> three:
+// four prompts of 2000 tokens, 16/8 heads, 84 -> 71, 16 of 1000 69 -> 72, two of
+// 6000 165 -> 185, 28/4 heads 267 -> 273; 16 rollouts 164 -> 169, 28/4 241 -> 250;
+// mixed, 48 decode steps beside a prompt of 1000, 16/8, 36.5 -> 32.3, 32 beside two
+// of 2000 65 -> 59, 16 beside 16 rollouts, 28/4, 250 -> 258.
 //
 // How a workgroup's rows are named: query rows of one head, (query row, head)
 // pairs of a KV head's group, or entries of a cascade's row list.
@@ -67,7 +75,10 @@ enum { kPoolSmall, kPoolLarge, kPool4 };
 // -> 34 us; 48 decode steps beside a prompt of 1000 tokens 52 -> 44, beside 64
 // chunks and an image of 4352 319 -> 310; 96 beside four prompts of 2500 and the
 // image 520 -> 491.  Spread evenly among the tiles instead, they took up to 50%
-// longer (a prompt's last tiles start late).
+// longer (a prompt's last tiles start late).  At d = 64, with the side stream -> in one
+// launch: 48 decode steps and a prompt of 1000 tokens, 16/8 heads, 48 -> 36.5 us, 28/4
+// 43.4 -> 34.2; 100 and four of 2000 108 -> 94, 28/4 123 -> 108; 4 and one of 1000, 28/4,
+// 38 either way; 16 and 16 rollouts 172 -> 165.
 __device__ __forceinline__ const KArgs& tile_args(const KArgs& a) { return a; }
 __device__ __forceinline__ const KArgs& tile_args(const MixedArgs& a) { return a.tile; }
 
