@@ -28,6 +28,7 @@ import ctypes
 import hashlib
 import json
 import os
+import struct
 import sys
 import time
 
@@ -47,16 +48,42 @@ BOUND = {"tiny_causal_f32": "alu", "decode_bf16": "hbm", "text_latent_bf16": "mf
 KERNEL_NAMES = ["tile_kernel", "few_kernel", "f32_kernel", "merge_kernel", "cascade_kernel"]
 DOMINANT = {"tiny_causal_f32": 2, "decode_bf16": 1, "text_latent_bf16": 0, "stream_window_bf16": 1,
             "rollout_bf16": 0, "cfg_labels_bf16": 0, "shared_prefix_decode_bf16": 1, "serving_mix_bf16": 0}
-KERNEL_SRC = [os.path.join(ROOT, "paper_2606_12688_amd", "csrc", f) for f in ("kernels.hip", "tile.h", "device.h")]
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "traffic.json")
 
 
-def kernel_source_sha() -> str:
-    sha = hashlib.sha256()
-    for src in KERNEL_SRC:
-        with open(src, "rb") as f:
-            sha.update(f.read())
-    return sha.hexdigest()[:16]
+def kernel_code_sha() -> str:
+    """Hash of the built device code of the kernels that this benchmark runs: the
+    code and kernel descriptors of the library's gfx950 code object that holds them
+    (the kernels of a 4-bit cache are in another).  Changes of other files, and of
+    comments, leave it as it is."""
+    from paper_2606_12688_amd import attn
+
+    with open(attn.LIB_PATH, "rb") as f:
+        lib = f.read()
+    magic = b"__CLANG_OFFLOAD_BUNDLE__"
+    at = lib.find(magic)
+    while at >= 0:
+        pos = at + len(magic) + 8
+        for _ in range(struct.unpack_from("<Q", lib, at + len(magic))[0]):
+            start, size, n = struct.unpack_from("<QQQ", lib, pos)
+            target = lib[pos + 24:pos + 24 + n]
+            pos += 24 + n
+            if not target.endswith(b"gfx950"):
+                continue
+            elf = lib[at + start:at + start + size]
+            if b"merge_kernel" not in elf:
+                continue
+            off, = struct.unpack_from("<Q", elf, 40)  # section headers, their size, number and names
+            step, count, names = struct.unpack_from("<HHH", elf, 58)
+            heads = [struct.unpack_from("<IIQQQQ", elf, off + step * i) for i in range(count)]
+            sha = hashlib.sha256()
+            for name, _, _, _, where, length in heads:
+                first = heads[names][4] + name
+                if elf[first:elf.index(b"\0", first)] in (b".text", b".rodata"):
+                    sha.update(elf[where:where + length])
+            return sha.hexdigest()[:16]
+        at = lib.find(magic, at + 1)
+    raise RuntimeError(f"{attn.LIB_PATH} holds no gfx950 code object with the attention kernels")
 
 
 def kv_bytes(b, key_ranges) -> int:
@@ -383,11 +410,11 @@ def bench_attention(args, name, dev, cpu_budget_s):
         achieved, peak, runit = flop / (k_mean * 1e-3) / 1e12, PEAK_FP32_TFLOPS, "TFLOP/s"
 
     traffic = None
-    traffic_note = "no counter run recorded for this kernel source"
+    traffic_note = "no counter run recorded for these kernels"
     if os.path.exists(TRAFFIC_FILE):
         with open(TRAFFIC_FILE) as f:
             rec = json.load(f).get(name + ("+cascade" if args.cascade else ""))
-        if rec and rec.get("kernel_src_sha") == kernel_source_sha():
+        if rec and rec.get("kernel_code_sha") == kernel_code_sha():
             traffic = rec["hbm_bytes_per_launch"]
             traffic_note = rec.get("note", "")
         elif rec:
