@@ -62,10 +62,11 @@ enum { kRows, kPacked, kCascade };
 // its D / 8 bytes of each record, and converts them into the same LDS image that
 // the direct loads of a 16-bit tile leave, so that each value is converted once
 // per workgroup and everything after it is the same.  Bound as the 16-bit instances
-// are (vector issue beside the matrix units): eight requests of 256 + 4096 tokens,
-// 28/4 heads at D = 128, take 1.71 ms, 1200 TFLOP/s, where those take 1.65; 64
-// rollouts of 768 rows at D = 64 526 us for 551; four prompts of 200-2000 tokens 56
-// either way.
+// are (vector issue beside the matrix units), with the conversions on top, and at D =
+// 64 LDS bank conflicts of the converted V (26 of a rollout's us).  In turn on one
+// card, on the same values, us with 16 -> 4 bits: eight requests of 256 + 4096 tokens,
+// 28/4 heads at D = 128, 1613 -> 1762 (1160 TFLOP/s); 64 rollouts of 768 rows at D = 64
+// 520 -> 588; four prompts of 200-2000 tokens 56 -> 59.
 enum { kPoolSmall, kPoolLarge, kPool4 };
 
 // FEW > 0: the launch also holds the few-row items of a 4-bit cache, of FEW 16-row
