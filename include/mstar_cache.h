@@ -49,8 +49,10 @@ extern "C" {
 /* mstar_kv_append for a 4-bit cache: the plan's new rows k_new / v_new
  * ([total_q][Hkv][head_dim] bf16, the row numbering of q) are rounded to 4 bits
  * and written to their places in the 4-bit pools k_pages / v_pages.  No other
- * key's codes or scales are written.  Pages, duplicate targets, targets outside
- * the pool, stream and capture as for mstar_kv_append.  Errors: INVALID_ARG
+ * key's codes or scales are written.  Pages, targets outside the pool, stream and
+ * capture as for mstar_kv_append; if two new rows target one slot, which they must
+ * not, its values are finite and otherwise unspecified (the codes of one may meet
+ * the scales of the other).  Errors: INVALID_ARG
  * (null or misaligned pointer, host-only plan, the plan's device is not the
  * current one), UNSUPPORTED (a plan of the fp32 dtype), HIP. */
 int mstar_kv4_append(const mstar_plan_t* plan, const void* k_new, const void* v_new, const int32_t* block_table,

@@ -146,8 +146,8 @@ def _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse):
 
 
 def kv4_fwd(pl: attn.Plan, q, k_pages, v_pages, block_table, out, lse, workspace=None, stream=None):
-    """``mstar_kv4_fwd`` on torch tensors: :func:`attn.fwd` over a 4-bit cache.
-    ``workspace`` as there (:func:`attn.workspace`)."""
+    """``mstar_kv4_fwd`` on torch tensors: :func:`attn.fwd` over a 4-bit cache, for
+    values of up to 2^64 in magnitude.  ``workspace`` as there (:func:`attn.workspace`)."""
     dev = _check_fwd(pl, q, k_pages, v_pages, block_table, out, lse)
     ws_ptr, ws_bytes = None, 0
     if workspace is not None:

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import workloads as W
-from oracle import block_tables, kv4_append
+from oracle import block_tables, kv4_append, kv4_read, kv4_values
 from paper_2606_12688_amd import attn, cache
 from tests.helpers import host64, plan_for
 from tests.kv4_helpers import DEV, compare4, queries, random_pools, reference, run_kv4
@@ -153,3 +153,28 @@ def test_a_cache_that_grows_step_by_step(d, hq, hkv):
         k4, v4 = kv4_append(b, host64(kn), host64(vn), k4, v4)
         assert np.array_equal(dk.cpu().numpy(), k4) and np.array_equal(dv.cpu().numpy(), v4)
         compare4(b, out, lse, reference(b, q, k4, v4), f"step {step} d{d}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_two_rows_for_one_slot_leave_finite_values_and_other_slots_alone(d):
+    import torch
+
+    b = W.custom("twice", 2, 2, d, [3, 3], [20, 20], [[(0, 20, C, 0)]] * 2, [0, 0], seed=1)
+    b.block_table[1] = b.block_table[0]  # both requests' rows go to slots 1-3 of one page
+    k4, v4 = random_pools(b, 1, poison=False)
+    g = torch.Generator(DEV).manual_seed(d)
+    kn, vn = ((torch.randn((6, 2, d), generator=g, device=DEV) * 2.0 ** 100).bfloat16() for _ in range(2))
+    kn[3:], vn[3:] = kn[3:] * 2.0 ** -180, vn[3:] * 2.0 ** -180
+    dk, dv, bt = _device(b, k4, v4)
+    pl = plan_for(b)
+    cache.kv4_append(pl, kn, vn, bt, dk, dv)
+    assert attn.check(pl) == 0
+    pl.destroy()
+    page, slots = b.block_table[0, 1], [1, 2, 3]
+    for which, got, old in (("k", dk, k4), ("v", dv, v4)):
+        now, before = (kv4_read(which, x, d) for x in (got.cpu().numpy(), old))
+        assert np.isfinite(kv4_values(*now)).all()
+        for x, y in zip(now, before):
+            x, y = x.copy(), y.copy()
+            x[page, slots] = y[page, slots] = 0
+            assert np.array_equal(x, y)
